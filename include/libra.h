@@ -357,6 +357,113 @@ int libra_csr_transpose_device(int64_t M, int64_t Kc, int64_t nnz, const int32_t
 int libra_csr_transpose_device_static(int64_t M, int64_t Kc, int64_t nnz, const int32_t *d_rowptr, const int32_t *d_col,
                                       int32_t *d_rowptr_t, int32_t *d_col_t, int32_t *d_perm_t, void *stream);
 
+/* ---- the ends of a training step: the rows it starts from, its loss, the update of its weights ----
+ *
+ * The sparse operators above are the middle of a training step (Section 5.5).  These calls are what stands around them.  They need no
+ * plan, launch on `stream`, wait for nothing and may be captured into a HIP graph.
+ */
+#define LIBRA_INDEX_I32 0
+#define LIBRA_INDEX_I64 1
+
+/*
+ * libra_embedding - out[i,:] = scale * table[index[i],:], formed in fp32 and rounded once to `dtype`.
+ *   table      device, rows x width with row stride ld_table elements (ld_table >= width), any type of values;  rows may be 0
+ *   index      device, n whole numbers (index_type).  -1 is padding: a row of zeros.  Any other number outside [0, rows) is a
+ *              mistake that no launch can refuse: its row becomes NaN
+ *   out        device, n x width with row stride ld_out; fully overwritten, what lies between the rows is left as it is; none of the inputs
+ * Errors: NULL, SHAPE, DTYPE, OPTION (index_type), BUFFER (an array not aligned to its elements), HIP.
+ */
+int libra_embedding(const void *table, int64_t rows, int32_t width, int64_t ld_table, int dtype, const void *index, int index_type,
+                    int64_t n, float scale, void *out, int64_t ld_out, void *stream);
+
+/*
+ * libra_embedding_backward - dtable[v,:] = scale * sum over all i with index[i] = v of dout[i,:]: the ids are sorted, the rows of an id
+ * are added in fp32, the sum is rounded once to `dtype`.  The order of additions depends on the ids and n alone, so equal calls give
+ * equal bits.  Rows that no id names become zeros; ids outside [0, rows) count for nothing.
+ *   dout       device, n x width with row stride ld_dout;  index as in libra_embedding;  n < 2^31
+ *   dtable     device, rows x width with row stride ld_dtable, rows < 2^31 - 1; fully overwritten; none of the inputs
+ *   workspace  device, 256-byte aligned, libra_embedding_backward_workspace() bytes, not needed after the call has run (n = 0: may be NULL)
+ * Errors: as libra_embedding, and TOO_LARGE; BUFFER also for the workspace.
+ */
+int libra_embedding_backward_workspace(int64_t n, int64_t rows, int32_t width, size_t *bytes);
+int libra_embedding_backward(const void *dout, int64_t ld_dout, int dtype, const void *index, int index_type, int64_t n, int64_t rows,
+                             int32_t width, float scale, void *dtable, int64_t ld_dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * libra_log_probs - for every row x of logits, with log p = log softmax(scale * x): the log probability of a given class, the entropy
+ * -sum p log p, and the `top` most likely classes with their log probabilities, in descending order of the logits (equal logits: lower
+ * class first).  All sums in fp32.
+ *   logits     device, n x classes with row stride ld elements, values of `dtype`;  n, classes < 2^31
+ *   targets    device, n classes (index_type), or NULL.  -1: none, log probability 0; another number outside [0, classes): NaN
+ *   top        0 .. LIBRA_LOG_PROBS_MAX_TOP and not above `classes`;  scale  finite, above 0
+ *   target_out, entropy  device, fp32[n];  top_out  fp32[n * top], top_index  int64[n * top] (NULL where targets or top are)
+ *   stats      device, fp32[2 n]: the largest logit and log sum exp(scale * (x - largest)) of each row, for the backward call
+ *   workspace  device, 256-byte aligned, libra_log_probs_workspace() bytes (0: may be NULL), not needed after the call has run
+ * A logit of -Inf is a class of probability 0.  A row of nothing else has no distribution: log probabilities -Inf, entropy 0, gradient 0.
+ * A row with a NaN or +Inf has NaN for all of its numbers; NaN counts as the largest logit.
+ * Errors: NULL, SHAPE, TOO_LARGE, UNSUPPORTED (top), DTYPE, OPTION (index_type, scale), BUFFER, HIP.
+ */
+#define LIBRA_LOG_PROBS_MAX_TOP 64
+int libra_log_probs_workspace(int64_t n, int64_t classes, int32_t top, size_t *bytes);
+int libra_log_probs(const void *logits, int64_t n, int64_t classes, int64_t ld, int dtype, const void *targets, int index_type,
+                    int32_t top, float scale, float *target_out, float *entropy, float *top_out, int64_t *top_index, float *stats,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * libra_log_probs_backward - gradient of libra_log_probs with respect to the logits, rounded once to their type:
+ * dlogits_j = scale * ([j = target] d + sum_a [j = top_index_a] d_a - p_j * (d + sum_a d_a + e * (log p_j + entropy))).
+ *   entropy, stats, top_index  what the forward call wrote for the same logits, targets, top and scale
+ *   d_target, d_entropy, d_top  device, fp32[n], fp32[n], fp32[n * top]: d, e and d_a above; each may be NULL (zeros)
+ *   dlogits    device, n x classes with row stride ld_dlogits, values of `dtype`; fully overwritten; none of the inputs
+ * Errors: as libra_log_probs.
+ */
+int libra_log_probs_backward(const void *logits, int64_t n, int64_t classes, int64_t ld, int dtype, const void *targets, int index_type,
+                             int32_t top, float scale, const float *entropy, const float *stats, const int64_t *top_index,
+                             const float *d_target, const float *d_entropy, const float *d_top, void *dlogits, int64_t ld_dlogits,
+                             void *stream);
+
+/*
+ * libra_adamw - one AdamW step over `count` tensors, in one launch for up to 32 tensors of a type:
+ *   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g g,   p <- (1 - lr wd) p - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * in fp32; a 16-bit parameter is rounded once, from p or from its copy in 32 bits where it has one (`master`, the number that is kept).
+ * state_bits = 32: m and v in fp32.  state_bits = 8: m and sqrt(v) as OCP e4m3 numbers, times a power of two (fp32, in first_scales and
+ * second_scales) for every LIBRA_ADAMW_BLOCK elements, the smallest that keeps the block's largest finite number within 448 (at least
+ * 2^-126).  The numbers that they stand for are rounded up or down to a neighbour by chance:
+ *   y = |x| / scale, e = max(exponent of y, -6), q = floor(y * 2^(3 - e) + chance), code = 8 (e + 6) + q
+ * with at least q = 1 for a root above 0; Inf and NaN become code 127.  The chance of element i of tensor `number`: h = mix(key + (low
+ * word of i) + (high word of i) * 0x9E3779B1), key = mix(mix(mix(seed) + t) + number), all modulo 2^32; (h mod 2^16) / 2^16 for m, (h div
+ * 2^16) / 2^16 for the root; mix(x): x ^= x >> 16, x *= 0x6C8E9CF5, x ^= x >> 15, x *= 0x58AC4D6B, x ^= x >> 16.  The same step gives
+ * the same bits every time.
+ *   tensors    host, read during the call.  Their arrays are on the device, n elements each without gaps, and do not overlap
+ *   opts       host.  step_dev, lr_dev: device, or NULL: then t and lr are read when the kernel runs, instead of `step` and `lr` (a
+ *              captured step counts on and follows a schedule)
+ * Errors: NULL, SHAPE, TOO_LARGE, DTYPE, OPTION, BUFFER (an array not aligned to its elements), HIP.  Nothing is changed by a call that
+ * is refused for its arguments.
+ */
+#define LIBRA_ADAMW_BLOCK 256
+typedef struct {
+    void       *param;          /* n values of dtype */
+    const void *grad;           /* n values of dtype */
+    void       *first;          /* m: n fp32 values, or n e4m3 codes */
+    void       *second;         /* v: n fp32 values, or n e4m3 codes of its root */
+    float      *first_scales;   /* 8 bits: ceil(n / LIBRA_ADAMW_BLOCK) powers of two */
+    float      *second_scales;
+    float      *master;         /* n fp32 values that `param` is the rounding of, or NULL */
+    int64_t     n;
+    int32_t     dtype;          /* LIBRA_F16, LIBRA_BF16 or LIBRA_F32 */
+    uint32_t    number;         /* which tensor this is, for the chances of 8-bit states */
+} libra_adamw_tensor_t;
+typedef struct {
+    uint32_t struct_size;       /* sizeof(libra_adamw_opts_t) */
+    int32_t  state_bits;        /* 32 or 8 */
+    double   lr, beta1, beta2, eps, weight_decay;   /* betas in [0, 1), eps >= 0 */
+    int64_t  step;              /* t, from 1 */
+    const int64_t *step_dev;
+    const float   *lr_dev;
+    uint32_t seed;
+} libra_adamw_opts_t;
+int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, const libra_adamw_opts_t *opts, void *stream);
+
 /*
  * libra_probe_coissue - the register-only concurrency experiment of Section 3.1 on this GPU: 1024 workgroups of 8 waves
  * (two per SIMD) run `iters` rounds of (a) 4 independent MFMA 16x16x16 chains on four of the waves, (b) 32 FMAs on

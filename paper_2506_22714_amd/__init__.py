@@ -7,4 +7,4 @@ Importing the package does not load the library; the first call does, and it
 raises if the library has not been built.
 """
 
-__all__ = ["binding", "workloads"]
+__all__ = ["autograd", "binding", "optim", "workloads"]

@@ -7,10 +7,18 @@ paper).  Only argument marshalling and the chain rule live here; every product r
                      dX = (A o dout) Y,  dY = (A o dout)^T X,  dA_p = dout_p <X_i, Y_j>
   alpha = softmax_row(scale * s)
                      ds_p = scale alpha_p (dalpha_p - sum_row alpha dalpha)
+
+and at the ends of a training step, before and behind the sparse layers:
+
+  out_i = scale W[index_i]
+                     dW_v = scale sum_{index_i = v} dout_i
+  log p = log softmax(scale x), H = -sum p log p
+                     dx_j = scale ([j = target] d + sum_a [j = top_a] d_a - p_j (d + sum_a d_a + e (log p_j + H)))
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as lb
 
@@ -129,3 +137,46 @@ def sddmm(sm: SparseMatrix, vals: torch.Tensor, X: torch.Tensor, Y: torch.Tensor
 def edge_softmax(sm: SparseMatrix, scores: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """Row-wise softmax of `scale * scores` over A's pattern; result in the matrix's value type."""
     return _EdgeSoftmax.apply(sm, scores, scale)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table: torch.Tensor, index: torch.Tensor, scale: float):
+        ctx.rows, ctx.scale = table.shape[0], scale
+        ctx.save_for_backward(index)
+        return lb.embedding(table.detach(), index, scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        (index,) = ctx.saved_tensors
+        return lb.embedding_backward(dout.reshape(-1, dout.shape[-1]).contiguous(), index, ctx.rows, ctx.scale), None, None
+
+
+class _LogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits: torch.Tensor, targets, top: int, scale: float):
+        r = lb.log_probs(logits.detach(), targets, top, scale)
+        ctx.scale = scale
+        ctx.save_for_backward(logits, targets, r.entropy, r.top_index, r.stats)
+        ctx.mark_non_differentiable(r.top_index)
+        ctx.set_materialize_grads(False)
+        return r.target, r.entropy, r.top, r.top_index
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_target, d_entropy, d_top, _):
+        logits, targets, entropy, top_index, stats = ctx.saved_tensors
+        parts = [None if d is None else d.float().contiguous() for d in (d_target, d_entropy, d_top)]
+        return lb.log_probs_backward(logits.detach(), lb.LogProbs(None, entropy, None, top_index, stats), targets, *parts, scale=ctx.scale), None, None, None
+
+
+def embedding(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """`scale * table[index]` in the table's type; -1 in `index` is padding: a row of zeros that has no gradient."""
+    return _Embedding.apply(table, index.contiguous(), scale)
+
+
+def log_probs(logits: torch.Tensor, targets: torch.Tensor | None = None, top: int = 0, scale: float = 1.0):
+    """(log probability of the given class, entropy, log probabilities of the `top` most likely classes, these classes) of every row of
+    `scale * logits`; all but the classes are fp32 and have gradients.  A target of -1 is none: 0, without a gradient."""
+    return _LogProbs.apply(logits, targets if targets is None else targets.contiguous(), top, scale)

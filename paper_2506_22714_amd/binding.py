@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -43,6 +44,27 @@ class PlanOpts(C.Structure):
     def __init__(self, **kw):
         super().__init__(**kw)
         self.struct_size = C.sizeof(PlanOpts)
+
+
+INDEX_I32, INDEX_I64 = 0, 1
+LOG_PROBS_MAX_TOP = 64
+ADAMW_BLOCK = 256
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("first", C.c_void_p), ("second", C.c_void_p),
+                ("first_scales", C.c_void_p), ("second_scales", C.c_void_p), ("master", C.c_void_p), ("n", C.c_int64),
+                ("dtype", C.c_int32), ("number", C.c_uint32)]
+
+
+class AdamwOpts(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("state_bits", C.c_int32), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p), ("lr_dev", C.c_void_p),
+                ("seed", C.c_uint32)]
+
+    def __init__(self, **kw):
+        super().__init__(**kw)
+        self.struct_size = C.sizeof(AdamwOpts)
 
 
 class Task(C.Structure):
@@ -110,6 +132,13 @@ def lib() -> C.CDLL:
         L.libra_sddmm_pattern_rounded.argtypes = [vp, vp, vp, i32, vp, vp]
         L.libra_edge_softmax_backward_rounded.argtypes = [vp, vp, vp, C.c_int, C.c_float, vp, vp]
         L.libra_value_products.argtypes = [vp, vp, i64, C.c_int, vp, vp]
+        L.libra_embedding.argtypes = [vp, i64, i32, i64, C.c_int, vp, C.c_int, i64, C.c_float, vp, i64, vp]
+        L.libra_embedding_backward_workspace.argtypes = [i64, i64, i32, C.POINTER(sz)]
+        L.libra_embedding_backward.argtypes = [vp, i64, C.c_int, vp, C.c_int, i64, i64, i32, C.c_float, vp, i64, vp, sz, vp]
+        L.libra_log_probs_workspace.argtypes = [i64, i64, i32, C.POINTER(sz)]
+        L.libra_log_probs.argtypes = [vp, i64, i64, i64, C.c_int, vp, C.c_int, i32, C.c_float, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.libra_log_probs_backward.argtypes = [vp, i64, i64, i64, C.c_int, vp, C.c_int, i32, C.c_float, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.libra_adamw.argtypes = [vp, i32, C.POINTER(AdamwOpts), vp]
         L.libra_probe_coissue.argtypes = [C.c_int, vp, C.POINTER(C.c_float * 3), vp]
         L.libra_probe_gather.argtypes = [vp, i64, i32, vp, i64, vp, vp]
         L.libra_probe_gather_hub.argtypes = [vp, i64, i32, vp, i64, vp, i32, vp, vp]
@@ -238,6 +267,49 @@ def libra_edge_softmax_backward(plan, alpha_ptr: int, alpha_dtype: int, dalpha_p
 def libra_value_products(vals_ptr: int, factors_ptr: int, n: int, dtype: int, out_ptr: int, stream: int = 0):
     _check(lib().libra_value_products(C.c_void_p(vals_ptr), C.c_void_p(factors_ptr), n, dtype, C.c_void_p(out_ptr), C.c_void_p(stream)),
            "libra_value_products")
+
+
+def libra_embedding(table_ptr: int, rows: int, width: int, ld_table: int, dtype: int, index_ptr: int, index_type: int, n: int, scale: float,
+                    out_ptr: int, ld_out: int, stream: int = 0):
+    _check(lib().libra_embedding(table_ptr, rows, width, ld_table, dtype, index_ptr, index_type, n, scale, out_ptr, ld_out, stream), "libra_embedding")
+
+
+def libra_embedding_backward_workspace(n: int, rows: int, width: int) -> int:
+    b = C.c_size_t()
+    _check(lib().libra_embedding_backward_workspace(n, rows, width, C.byref(b)), "libra_embedding_backward_workspace")
+    return int(b.value)
+
+
+def libra_embedding_backward(dout_ptr: int, ld_dout: int, dtype: int, index_ptr: int, index_type: int, n: int, rows: int, width: int,
+                             scale: float, dtable_ptr: int, ld_dtable: int, ws_ptr: int, ws_bytes: int, stream: int = 0):
+    _check(lib().libra_embedding_backward(dout_ptr, ld_dout, dtype, index_ptr, index_type, n, rows, width, scale, dtable_ptr, ld_dtable,
+                                          ws_ptr, ws_bytes, stream), "libra_embedding_backward")
+
+
+def libra_log_probs_workspace(n: int, classes: int, top: int) -> int:
+    b = C.c_size_t()
+    _check(lib().libra_log_probs_workspace(n, classes, top, C.byref(b)), "libra_log_probs_workspace")
+    return int(b.value)
+
+
+def libra_log_probs(logits_ptr: int, n: int, classes: int, ld: int, dtype: int, targets_ptr: int, index_type: int, top: int, scale: float,
+                    target_ptr: int, entropy_ptr: int, top_ptr: int, top_index_ptr: int, stats_ptr: int, ws_ptr: int = 0, ws_bytes: int = 0,
+                    stream: int = 0):
+    _check(lib().libra_log_probs(logits_ptr, n, classes, ld, dtype, targets_ptr, index_type, top, scale, target_ptr, entropy_ptr, top_ptr,
+                                 top_index_ptr, stats_ptr, ws_ptr, ws_bytes, stream), "libra_log_probs")
+
+
+def libra_log_probs_backward(logits_ptr: int, n: int, classes: int, ld: int, dtype: int, targets_ptr: int, index_type: int, top: int,
+                             scale: float, entropy_ptr: int, stats_ptr: int, top_index_ptr: int, d_target_ptr: int, d_entropy_ptr: int,
+                             d_top_ptr: int, dlogits_ptr: int, ld_dlogits: int, stream: int = 0):
+    _check(lib().libra_log_probs_backward(logits_ptr, n, classes, ld, dtype, targets_ptr, index_type, top, scale, entropy_ptr, stats_ptr,
+                                          top_index_ptr, d_target_ptr, d_entropy_ptr, d_top_ptr, dlogits_ptr, ld_dlogits, stream),
+           "libra_log_probs_backward")
+
+
+def libra_adamw(tensors, count: int, opts: AdamwOpts, stream: int = 0):
+    """`tensors`: a ctypes array of :class:`AdamwTensor`."""
+    _check(lib().libra_adamw(tensors, count, C.byref(opts), stream), "libra_adamw")
 
 
 def libra_probe_coissue(iters: int, sink_ptr: int, stream: int = 0):
@@ -719,3 +791,246 @@ class Plan:
                                                      scratch.data_ptr() if scratch is not None else 0, _stream())
         if rc:
             _check(rc, "libra_plan_set_values_ordered")
+
+
+# ---- the ends of a training step: no plan, any GPU (the call is made on the device and the current stream of its operands) ----
+def _launch(call, what: str, like, *args):
+    """call(*args, stream) on the device of the tensor `like`."""
+    torch = _torch
+    if like.get_device() == torch.cuda.current_device():
+        rc = call(*args, _stream())
+    else:
+        with torch.cuda.device(like.device):
+            rc = call(*args, torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc, what)
+
+
+def _code(t, name: str) -> int:
+    torch = _torch
+    d = t.dtype if isinstance(t, torch.Tensor) else None
+    if d is torch.float16:
+        return F16
+    if d is torch.bfloat16:
+        return BF16
+    if d is torch.float32:
+        return F32
+    raise ValueError(f"{name}: expected a torch tensor of float16, bfloat16 or float32, got {d or type(t).__name__}")
+
+
+def _rows_of(t, name: str, cols=None, like=None) -> int:
+    """A matrix whose rows are contiguous (with any distance between them); its type's code."""
+    code = _code(t, name)
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ('*', {'*' if cols is None else cols})")
+    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows must be contiguous (strides {tuple(t.stride())})")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a GPU tensor")
+    if like is not None and (t.get_device() != like.get_device() or t.dtype is not like.dtype):
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    return code
+
+
+def _ld(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _index_code(t, name: str, like) -> int:
+    torch = _torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous int32 or int64 torch tensor")
+    if not t.is_cuda or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: must be a tensor on {like.device}")
+    return INDEX_I64 if t.dtype is torch.int64 else INDEX_I32
+
+
+def _fp32_on(t, name: str, shape, like):
+    torch = _torch
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous float32 torch tensor of shape {tuple(shape)}")
+    if not t.is_cuda or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: must be a tensor on {like.device}")
+    return t.data_ptr()
+
+
+def embedding(table, index, scale: float = 1.0, out=None):
+    """``scale * table[index]`` in the table's type, rounded once.  ``index`` (int32 or int64, any shape): -1 is padding, a row of zeros;
+    another number outside the table gives a row of NaN.  ``out``: matrix of index.numel() rows to write to."""
+    torch = _gpu()
+    dtype = _rows_of(table, "table")
+    kind = _index_code(index, "index", table)
+    n, (rows, width) = index.numel(), table.shape
+    if width < 1:
+        raise ValueError("table: rows of no elements")
+    if out is None:
+        out = torch.empty((n, width), dtype=table.dtype, device=table.device)
+        result = out.view(*index.shape, width)
+    else:
+        _rows_of(out, "out", width, like=table)
+        if out.shape[0] != n:
+            raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+        result = out
+    _launch(lib().libra_embedding, "libra_embedding", table, table.data_ptr(), rows, width, _ld(table), dtype, index.data_ptr(), kind, n, scale,
+            out.data_ptr(), _ld(out))
+    return result
+
+
+def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
+    """Gradient of ``embedding(table, index, scale)`` with respect to a table of ``rows`` rows, from the gradient ``dout`` (a row per id)
+    of its result: rows of equal ids are added in fp32, in an order that depends on the ids alone, and rounded once to dout's type."""
+    torch = _gpu()
+    dtype = _rows_of(dout, "dout")
+    kind = _index_code(index, "index", dout)
+    n, width = dout.shape
+    if width < 1:
+        raise ValueError("dout: rows of no elements")
+    if index.numel() != n:
+        raise ValueError(f"index: {index.numel()} ids for {n} rows of dout")
+    if out is None:
+        out = torch.empty((rows, width), dtype=dout.dtype, device=dout.device)
+    else:
+        _rows_of(out, "out", width, like=dout)
+        if out.shape[0] != rows:
+            raise ValueError(f"out: {out.shape[0]} rows, expected {rows}")
+    nb = libra_embedding_backward_workspace(n, rows, width)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dout.device)
+    _launch(lib().libra_embedding_backward, "libra_embedding_backward", dout, dout.data_ptr(), _ld(dout), dtype, index.data_ptr(), kind, n, rows,
+            width, scale, out.data_ptr(), _ld(out), ws.data_ptr(), nb)
+    return out
+
+
+class LogProbs(NamedTuple):
+    """What :func:`log_probs` gives for n rows of logits: log probability of the given class (None without targets) and entropy, fp32[n];
+    the ``top`` most likely classes, int64[n, top], and their log probabilities, fp32[n, top]; ``stats`` is for the backward call."""
+    target: object
+    entropy: object
+    top: object
+    top_index: object
+    stats: object
+
+
+def log_probs(logits, targets=None, top: int = 0, scale: float = 1.0) -> LogProbs:
+    """Log softmax of ``scale * logits`` at the given classes (-1: none, 0), its entropy and its ``top`` largest entries."""
+    torch = _gpu()
+    dtype = _rows_of(logits, "logits")
+    n, classes = logits.shape
+    kind = 0
+    if targets is not None:
+        kind = _index_code(targets, "targets", logits)
+        if targets.shape != (n,):
+            raise ValueError(f"targets: shape {tuple(targets.shape)}, expected ({n},)")
+    nb = libra_log_probs_workspace(n, classes, top)
+    device = logits.device
+    target = torch.empty(n, dtype=torch.float32, device=device) if targets is not None else None
+    entropy = torch.empty(n, dtype=torch.float32, device=device)
+    stats = torch.empty((n, 2), dtype=torch.float32, device=device)
+    best = torch.empty((n, top), dtype=torch.float32, device=device)
+    index = torch.empty((n, top), dtype=torch.int64, device=device)
+    ws = torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+    _launch(lib().libra_log_probs, "libra_log_probs", logits, logits.data_ptr(), n, classes, _ld(logits), dtype,
+            targets.data_ptr() if targets is not None else 0, kind, top, scale, target.data_ptr() if targets is not None else 0,
+            entropy.data_ptr(), best.data_ptr(), index.data_ptr(), stats.data_ptr(), ws.data_ptr() if nb else 0, nb)
+    return LogProbs(target, entropy, best, index, stats)
+
+
+def log_probs_backward(logits, result: LogProbs, targets=None, d_target=None, d_entropy=None, d_top=None, scale: float = 1.0, out=None):
+    """Gradient of :func:`log_probs` (its ``result`` for the same logits, targets and scale) with respect to the logits, in their type, from
+    the gradients of the target's log probabilities, the entropies and the alternatives' log probabilities (None: zero)."""
+    torch = _gpu()
+    dtype = _rows_of(logits, "logits")
+    n, classes = logits.shape
+    top = result.top_index.shape[1]
+    kind = 0
+    if targets is not None:
+        kind = _index_code(targets, "targets", logits)
+        if targets.shape != (n,):
+            raise ValueError(f"targets: shape {tuple(targets.shape)}, expected ({n},)")
+    if d_target is not None and targets is None:
+        raise ValueError("d_target: without targets")
+    entropy, stats = _fp32_on(result.entropy, "entropy", (n,), logits), _fp32_on(result.stats, "stats", (n, 2), logits)
+    if _index_code(result.top_index, "top_index", logits) != INDEX_I64 or result.top_index.shape[0] != n:
+        raise ValueError(f"top_index: expected int64 of shape ({n}, top)")
+    grads = [0 if t is None else _fp32_on(t, name, want, logits)
+             for t, name, want in ((d_target, "d_target", (n,)), (d_entropy, "d_entropy", (n,)), (d_top, "d_top", (n, top)))]
+    if out is None:
+        out = torch.empty((n, classes), dtype=logits.dtype, device=logits.device)
+    else:
+        _rows_of(out, "out", classes, like=logits)
+        if out.shape[0] != n:
+            raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+    _launch(lib().libra_log_probs_backward, "libra_log_probs_backward", logits, logits.data_ptr(), n, classes, _ld(logits), dtype,
+            targets.data_ptr() if targets is not None else 0, kind, top, scale, entropy, stats, result.top_index.data_ptr(), *grads,
+            out.data_ptr(), _ld(out))
+    return out
+
+
+def _adamw_array(t, name: str, k: int, dtype, n: int, device: int) -> int:
+    if not isinstance(t, _torch.Tensor) or t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        what = f"{t.dtype}, {t.numel()} elements, contiguous: {t.is_contiguous()}, {t.device}" if isinstance(t, _torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name}[{k}]: {what}; expected contiguous {dtype} of {n} elements on GPU {device}")
+    return t.data_ptr()
+
+
+def _one_on(x, name: str, dtype, like) -> int:
+    """Address of a number that is read on the device when the kernel runs."""
+    if x.dtype is not dtype or x.numel() != 1 or x.get_device() != like.get_device():
+        raise ValueError(f"{name}: expected one {dtype} on {like.device}")
+    return x.data_ptr()
+
+
+def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
+          first_scales=None, second_scales=None, masters=None, seed: int = 0, numbers=None):
+    """One AdamW step, in place, over lists of contiguous tensors on one GPU.
+
+    ``first``, ``second``: m and v of each parameter in float32; or, with ``first_scales`` and ``second_scales`` (a float32 for every
+    ADAMW_BLOCK elements, all given together), m and sqrt(v) in 8 bits, as float8_e4m3fn.  ``masters``: the parameters in float32, of
+    which the 16-bit ones are the roundings (a list, None where a tensor has none).  ``step`` counts from 1.  ``step`` and ``lr`` may be
+    one-element tensors on the GPU (int64, float32): they are read when the kernel runs, also of a captured step.  ``seed``, ``numbers``
+    (of the tensors; their places in the list): of the chances by which 8-bit states are rounded."""
+    torch = _gpu()
+    count = len(params)
+    bits8 = first_scales is not None
+    if bits8 != (second_scales is not None):
+        raise ValueError("first_scales and second_scales go together")
+    for name, x in (("grads", grads), ("first", first), ("second", second), ("first_scales", first_scales), ("second_scales", second_scales),
+                    ("masters", masters), ("numbers", numbers)):
+        if x is not None and len(x) != count:
+            raise ValueError(f"{name}: {len(x)} tensors for {count} parameters")
+    if count == 0:
+        return
+    state = torch.float8_e4m3fn if bits8 else torch.float32
+    device = params[0].get_device()
+    if device < 0:
+        raise ValueError("params[0]: must be a GPU tensor")
+    table = (AdamwTensor * count)()
+    seen = set()
+    for k, p in enumerate(params):
+        code, n = _code(p, f"params[{k}]"), p.numel()
+        r = table[k]
+        r.param = _adamw_array(p, "params", k, p.dtype, n, device)
+        r.grad = _adamw_array(grads[k], "grads", k, p.dtype, n, device)
+        r.first = _adamw_array(first[k], "first", k, state, n, device)
+        r.second = _adamw_array(second[k], "second", k, state, n, device)
+        if bits8:
+            blocks = -(-n // ADAMW_BLOCK)
+            r.first_scales = _adamw_array(first_scales[k], "first_scales", k, torch.float32, blocks, device)
+            r.second_scales = _adamw_array(second_scales[k], "second_scales", k, torch.float32, blocks, device)
+        if masters is not None and masters[k] is not None:
+            r.master = _adamw_array(masters[k], "masters", k, torch.float32, n, device)
+        r.n, r.dtype, r.number = n, code, k if numbers is None else numbers[k]
+        if n:
+            if r.param in seen:
+                raise ValueError(f"params[{k}]: the same tensor twice")
+            seen.add(r.param)
+    opts = AdamwOpts(state_bits=8 if bits8 else 32, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=seed & 0xffffffff)
+    if isinstance(step, torch.Tensor):
+        opts.step_dev = _one_on(step, "step", torch.int64, params[0])
+    else:
+        opts.step = step
+    if isinstance(lr, torch.Tensor):
+        opts.lr_dev = _one_on(lr, "lr", torch.float32, params[0])
+    else:
+        opts.lr = lr
+    _launch(lib().libra_adamw, "libra_adamw", params[0], table, count, C.byref(opts))
+    torch.autograd.graph.increment_version(params)           # a graph that saved one of them must notice

@@ -1,0 +1,181 @@
+"""A whole training step of a small graph network as a program runs it: rows of a learned table -> an aggregation on the graph -> attention
+on the graph -> classes -> loss with an entropy bonus -> gradients -> AdamW, against the same in 64 bits on dense matrices."""
+import numpy as np
+import pytest
+
+from paper_2506_22714_amd import binding as lb
+from paper_2506_22714_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lb.lib()
+
+
+def setup(seed=0):
+    A = wl.random_pattern(300, 300, 0.05, seed=4, empty_rows=0.1)
+    rng = np.random.default_rng(seed)
+    ids = rng.integers(0, 120, 300)                    # several nodes share a row of the table
+    ids[::50] = -1
+    targets = rng.integers(0, 10, 300)
+    targets[::7] = -1
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()      # noqa: E731
+    table = dev((0.5 * rng.standard_normal((120, 32))).astype(np.float32))
+    head = dev((0.3 * rng.standard_normal((32, 10))).astype(np.float32))
+    return A, dev(ids), dev(targets), table, head
+
+
+def loss_of(logp, h, given):
+    return -logp.sum() / given - 0.05 * h.mean()
+
+
+def ours(sm, vals, ids, targets, table, head):
+    from paper_2506_22714_amd import autograd as ag
+    x = ag.embedding(table, ids, scale=1.5)
+    x = ag.spmm(sm, vals, x)
+    s = ag.sddmm(sm, torch.ones_like(vals), x, x)
+    x = ag.spmm(sm, ag.edge_softmax(sm, s, 0.2), x)
+    logp, h, top, classes = ag.log_probs(x @ head, targets, top=3, scale=2.0)
+    return loss_of(logp, h, (targets >= 0).sum()), top, classes
+
+
+def plain(A, vals, ids, targets, table, head):
+    dense = torch.zeros(A.M, A.Kc, dtype=torch.float64, device="cuda")
+    rows = torch.from_numpy(np.repeat(np.arange(A.M), np.diff(A.rowptr))).cuda()
+    cols = torch.from_numpy(A.col.astype(np.int64)).cuda()
+    dense = dense.index_put((rows, cols), vals.double())
+    there = torch.zeros_like(dense, dtype=torch.bool).index_put((rows, cols), torch.tensor(True, device="cuda"))
+    x = torch.where((ids < 0)[:, None], 0.0, 1.5 * table[ids.clamp(min=0)])
+    x = dense @ x
+    s = torch.where(there, 0.2 * (x @ x.t()), -torch.inf)
+    some = there.any(1, keepdim=True)
+    alpha = torch.where(there, torch.softmax(torch.where(some, s, 0.0), 1), 0.0)
+    x = alpha @ x
+    logp = torch.log_softmax(2.0 * (x @ head), 1)
+    h = -(logp.exp() * logp).sum(1)
+    given = torch.where(targets >= 0, logp.gather(1, targets.clamp(min=0)[:, None])[:, 0], 0.0)
+    return loss_of(given, h, (targets >= 0).sum())
+
+
+def make(A):
+    from paper_2506_22714_amd import autograd as ag
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()      # noqa: E731
+    return ag.SparseMatrix(A.M, A.Kc, dev(A.rowptr), dev(A.col), dtype=torch.float32)
+
+
+def test_gradients_and_update_of_a_whole_step():
+    from paper_2506_22714_amd.optim import AdamW
+    A, ids, targets, table, head = setup()
+    sm = make(A)
+    vals = torch.from_numpy(A.val.astype(np.float32)).cuda()
+    ps = [torch.nn.Parameter(table.clone()), torch.nn.Parameter(head.clone())]
+    qs = [table.double().requires_grad_(), head.double().requires_grad_()]
+    opt = AdamW(ps, lr=1e-2, weight_decay=0.1)
+    for step in range(3):
+        opt.zero_grad()
+        loss, _, _ = ours(sm, vals, ids, targets, *ps)
+        loss.backward()
+        for q, p in zip(qs, ps):
+            q.grad = None
+            q.data = p.detach().double()
+        want = plain(A, vals, ids, targets, *qs)
+        want.backward()
+        assert abs(float(loss) - float(want)) < 1e-4 * max(1.0, abs(float(want)))
+        for p, q in zip(ps, qs):
+            # sums of some hundred fp32 terms, five products deep: 2^-24 * 100 * 5 of the gradients' size
+            size = float(q.grad.abs().max())
+            assert float((p.grad.double() - q.grad).abs().max()) < 2.0 ** -24 * 500 * 4 * size
+        before = [p.detach().double() for p in ps]
+        grads = [p.grad.double() for p in ps]
+        if step == 0:
+            states = [[torch.zeros_like(g), torch.zeros_like(g)] for g in grads]
+        opt.step()
+        for p, b, g, s in zip(ps, before, grads, states):
+            s[0] = 0.9 * s[0] + 0.1 * g
+            s[1] = 0.999 * s[1] + 0.001 * g * g
+            new = b * (1 - 1e-2 * 0.1) - 1e-2 * (s[0] / (1 - 0.9 ** (step + 1))) / ((s[1] / (1 - 0.999 ** (step + 1))).sqrt() + 1e-8)
+            # some forty roundings of 2^-24 of steps of 1e-2, the parameter's own; the eps of 1e-8 keeps the quotient steady
+            assert float((p.detach().double() - new).abs().max()) < 2.0 ** -24 * (2 * float(new.abs().max()) + 4 * 40 * 1e-2)
+    sm.close()
+
+
+def test_a_whole_step_replayed_from_a_graph():
+    """The captured step against the eager one, from the same weights, three times in a row."""
+    from paper_2506_22714_amd.optim import AdamW
+    A, ids, targets, table, head = setup(1)
+    sm = make(A)
+    vals = torch.from_numpy(A.val.astype(np.float32)).cuda()
+    runs = []
+    for captured in (False, True):
+        ps = [torch.nn.Parameter(table.clone()), torch.nn.Parameter(head.clone())]
+        opt = AdamW(ps, lr=1e-2, state_bits=8, capturable=captured)
+        def step():
+            opt.zero_grad(set_to_none=True)
+            loss, _, _ = ours(sm, vals, ids, targets, *ps)
+            loss.backward()
+            opt.step()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        seen = []
+        for _ in range(3):
+            graph.replay() if captured else step()
+            torch.cuda.synchronize()
+            seen.append([p.detach().clone() for p in ps])
+        runs.append(seen)
+    for eager, replayed in zip(*runs):
+        for a, b in zip(eager, replayed):
+            # Steps of 1e-2.  Atomic sums of the aggregation differ in their last places between runs: a gradient near zero may turn its
+            # sign, and a state's rounding its direction (an eighth of it); few elements meet either
+            assert float((a - b).abs().mean()) < 1e-3
+    sm.close()
+
+
+def test_no_second_derivatives():
+    from paper_2506_22714_amd import autograd as ag
+    w = torch.randn(5, 4, device="cuda", requires_grad=True)
+    ids = torch.tensor([1, 1, -1], device="cuda")
+    (g,) = torch.autograd.grad((ag.embedding(w, ids) ** 2).sum(), w, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_broadcast_and_strided_gradients():
+    from paper_2506_22714_amd import autograd as ag
+    w = torch.randn(6, 8, device="cuda", requires_grad=True)
+    ids = torch.tensor([[1, 1], [0, -1], [5, 1]], device="cuda")
+    ag.embedding(w, ids, scale=2.0).sum().backward()            # a gradient of one element, expanded
+    want = torch.zeros(6, 8, device="cuda")
+    want[1], want[0], want[5] = 6.0, 2.0, 2.0
+    assert torch.equal(w.grad, want)
+    w.grad = None
+    u = torch.randn(8, 3, 2, device="cuda")
+    (ag.embedding(w, ids).permute(2, 0, 1) * u).sum().backward()
+    want = torch.zeros(6, 8, device="cuda", dtype=torch.float64)
+    for a in range(3):
+        for b in range(2):
+            if ids[a, b] >= 0:
+                want[ids[a, b]] += u[:, a, b].double()
+    assert float((w.grad.double() - want).abs().max()) < 4 * 2.0 ** -24 * 10
+    x = torch.randn(4, 9, device="cuda", requires_grad=True)
+    logp, h, top, classes = ag.log_probs(x.t()[:, :].contiguous(), torch.tensor([0, 1, 2, 3, 0, 1, 2, 3, -1], device="cuda"), top=2)
+    (logp.sum() + h[::2].sum() + top.t()[0].sum()).backward()
+    z = x.detach().double().requires_grad_()
+    lp = torch.log_softmax(z.t(), 1)
+    ref = lp[torch.arange(8), torch.arange(8) % 4].sum() - (lp.exp() * lp).sum(1)[::2].sum() + lp.amax(1).sum()
+    ref.backward()
+    assert float((x.grad.double() - z.grad).abs().max()) < 2.0 ** -24 * 400
+    assert not classes.requires_grad

@@ -1,0 +1,144 @@
+"""What the calls at the ends of a training step refuse, through the C ABI (arguments are looked at before anything touches a GPU) and
+through the binding."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_22714_amd import binding as lb
+
+OK, E = lb.OK, lb.ERR
+BUF = np.zeros(4096, dtype=np.uint8)
+AT = -(-BUF.ctypes.data // 256) * 256           # never read or written: every call here is refused, or has nothing to do
+
+
+def embedding(**kw):
+    a = dict(table=AT, rows=4, width=8, ld_table=8, dtype=lb.F16, index=AT, index_type=lb.INDEX_I64, n=2, scale=1.0, out=AT, ld_out=8)
+    a.update(kw)
+    return lb.lib().libra_embedding(*a.values(), None)
+
+
+def scatter(**kw):
+    a = dict(dout=AT, ld_dout=8, dtype=lb.F16, index=AT, index_type=lb.INDEX_I64, n=2, rows=4, width=8, scale=1.0, out=AT, ld_out=8, ws=AT, ws_bytes=1 << 30)
+    a.update(kw)
+    return lb.lib().libra_embedding_backward(*a.values(), None)
+
+
+def log_probs(**kw):
+    a = dict(logits=AT, n=2, classes=8, ld=8, dtype=lb.F32, targets=AT, index_type=lb.INDEX_I64, top=2, scale=1.0, target_out=AT, entropy=AT,
+             top_out=AT, top_index=AT, stats=AT, ws=AT, ws_bytes=1 << 30)
+    a.update(kw)
+    return lb.lib().libra_log_probs(*a.values(), None)
+
+
+def log_probs_backward(**kw):
+    a = dict(logits=AT, n=2, classes=8, ld=8, dtype=lb.F32, targets=AT, index_type=lb.INDEX_I64, top=2, scale=1.0, entropy=AT, stats=AT,
+             top_index=AT, d_target=AT, d_entropy=AT, d_top=AT, out=AT, ld_out=8)
+    a.update(kw)
+    return lb.lib().libra_log_probs_backward(*a.values(), None)
+
+
+def adamw(bits=32, tensors=None, count=None, opts=True, **kw):
+    o = lb.AdamwOpts(state_bits=bits, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0, step=1)
+    t = dict(param=AT, grad=AT, first=AT, second=AT, first_scales=AT, second_scales=AT, n=4, dtype=lb.F32)
+    for k, v in kw.items():
+        if k in t or k in ("master", "number"):
+            t[k] = v
+        else:
+            setattr(o, k, v)
+    table = (lb.AdamwTensor * 1)(lb.AdamwTensor(**t)) if tensors is None else tensors
+    return lb.lib().libra_adamw(table, 1 if count is None else count, C.byref(o) if opts else None, None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    ("SHAPE", dict(n=-1)), ("SHAPE", dict(rows=-1)), ("SHAPE", dict(width=0)), ("SHAPE", dict(ld_table=7)), ("SHAPE", dict(ld_out=7)),
+    ("DTYPE", dict(dtype=3)), ("OPTION", dict(index_type=2)), ("NULL", dict(table=None)), ("NULL", dict(index=None)), ("NULL", dict(out=None)),
+    ("BUFFER", dict(table=AT + 1)), ("BUFFER", dict(index=AT + 4)), ("BUFFER", dict(out=AT + 1)), ("BUFFER", dict(dtype=lb.F32, out=AT + 2)),
+])
+def test_embedding_refuses(want, kw):
+    assert embedding(**kw) == E[want]
+
+
+@pytest.mark.parametrize("want,kw", [
+    ("SHAPE", dict(n=-1)), ("SHAPE", dict(rows=-1)), ("SHAPE", dict(width=0)), ("SHAPE", dict(ld_dout=7)), ("SHAPE", dict(ld_out=7)),
+    ("TOO_LARGE", dict(n=1 << 31)), ("TOO_LARGE", dict(rows=(1 << 31) - 1)), ("DTYPE", dict(dtype=-1)), ("OPTION", dict(index_type=-1)),
+    ("NULL", dict(dout=None)), ("NULL", dict(index=None)), ("NULL", dict(out=None)), ("NULL", dict(ws=None)),
+    ("BUFFER", dict(ws=AT + 128)), ("BUFFER", dict(ws_bytes=8)), ("BUFFER", dict(dout=AT + 1)), ("BUFFER", dict(index=AT + 4)), ("BUFFER", dict(out=AT + 1)),
+])
+def test_embedding_backward_refuses(want, kw):
+    assert scatter(**kw) == E[want]
+
+
+@pytest.mark.parametrize("want,kw", [
+    ("SHAPE", dict(n=-1)), ("SHAPE", dict(classes=0, ld=0, top=0)), ("SHAPE", dict(ld=7)), ("SHAPE", dict(top=-1)), ("SHAPE", dict(top=9)),
+    ("TOO_LARGE", dict(n=1 << 31)), ("TOO_LARGE", dict(classes=1 << 31, ld=1 << 31)), ("UNSUPPORTED", dict(classes=100, ld=100, top=65)),
+    ("DTYPE", dict(dtype=3)), ("OPTION", dict(index_type=2)), ("OPTION", dict(scale=0.0)), ("OPTION", dict(scale=-1.0)),
+    ("OPTION", dict(scale=float("inf"))), ("OPTION", dict(scale=float("nan"))), ("NULL", dict(logits=None)), ("BUFFER", dict(logits=AT + 2)),
+    ("BUFFER", dict(targets=AT + 4)), ("NULL", dict(entropy=None)), ("NULL", dict(stats=None)), ("NULL", dict(top_index=None)),
+    ("BUFFER", dict(top_index=AT + 4)), ("BUFFER", dict(entropy=AT + 2)), ("BUFFER", dict(stats=AT + 2)),
+])
+def test_log_probs_refuse_both_ways(want, kw):
+    assert log_probs(**kw) == E[want]
+    assert log_probs_backward(**kw) == E[want]
+
+
+def test_log_probs_refuse_one_way():
+    assert log_probs(target_out=None) == E["NULL"]
+    assert log_probs(top_out=None) == E["NULL"]
+    assert log_probs(top_out=AT + 2) == E["BUFFER"]
+    assert log_probs_backward(ld_out=7) == E["SHAPE"]
+    assert log_probs_backward(out=None) == E["NULL"]
+    assert log_probs_backward(targets=None) == E["NULL"]            # a gradient of targets that are not there
+    for name in ("d_target", "d_entropy", "d_top"):
+        assert log_probs_backward(**{name: AT + 2}) == E["BUFFER"]
+
+
+@pytest.mark.parametrize("want,kw", [
+    ("SHAPE", dict(n=-1)), ("SHAPE", dict(count=-1)), ("NULL", dict(opts=False)), ("DTYPE", dict(dtype=3)), ("OPTION", dict(struct_size=4)),
+    ("OPTION", dict(state_bits=16)), ("OPTION", dict(beta1=1.0)), ("OPTION", dict(beta1=-0.1)), ("OPTION", dict(beta2=1.0)), ("OPTION", dict(beta2=float("nan"))),
+    ("OPTION", dict(eps=-1.0)), ("OPTION", dict(eps=float("inf"))), ("OPTION", dict(lr=float("nan"))), ("OPTION", dict(weight_decay=float("inf"))),
+    ("OPTION", dict(step=0)), ("BUFFER", dict(step_dev=AT + 4)), ("BUFFER", dict(lr_dev=AT + 2)), ("TOO_LARGE", dict(n=1 << 60)),
+    ("NULL", dict(param=None)), ("NULL", dict(grad=None)), ("NULL", dict(first=None)), ("NULL", dict(second=None)),
+    ("NULL", dict(bits=8, first_scales=None)), ("NULL", dict(bits=8, second_scales=None)), ("BUFFER", dict(param=AT + 2)), ("BUFFER", dict(grad=AT + 1)),
+    ("BUFFER", dict(first=AT + 2)), ("BUFFER", dict(second=AT + 1)), ("BUFFER", dict(master=AT + 2)), ("BUFFER", dict(bits=8, first_scales=AT + 2)),
+])
+def test_adamw_refuses(want, kw):
+    assert adamw(**kw) == E[want]
+
+
+def test_nothing_to_do_is_no_error():
+    assert embedding(n=0, table=None, index=None, out=None) == OK
+    assert scatter(rows=0, dout=None, index=None, out=None, ws=None) == OK
+    assert log_probs(n=0, logits=None, targets=None, target_out=None, entropy=None, top_out=None, top_index=None, stats=None) == OK
+    assert log_probs_backward(n=0, logits=None, out=None) == OK
+    assert adamw(count=0) == OK
+    assert adamw(n=0, param=None, grad=None, first=None, second=None) == OK
+    n = C.c_size_t()
+    assert lb.lib().libra_embedding_backward_workspace(5, 1 << 31, 4, C.byref(n)) == E["TOO_LARGE"]
+    assert lb.lib().libra_embedding_backward_workspace(5, 10, 4, None) == E["NULL"]
+    assert lb.lib().libra_log_probs_workspace(5, 10, 11, C.byref(n)) == E["SHAPE"]
+    assert lb.lib().libra_log_probs_workspace(5, 10, 4, None) == E["NULL"]
+
+
+def test_the_binding_wants_gpu_tensors_of_the_right_kind():
+    table, ids = torch.zeros(4, 8), torch.zeros(3, dtype=torch.int64)
+    for call in (lambda: lb.embedding(table, ids), lambda: lb.embedding(table.double(), ids), lambda: lb.embedding(table[0], ids),
+                 lambda: lb.embedding(table.t(), ids), lambda: lb.embedding([1.0], ids), lambda: lb.embedding_backward(table, ids, 5),
+                 lambda: lb.log_probs(table), lambda: lb.log_probs(table.int()), lambda: lb.log_probs_backward(table, None)):
+        with pytest.raises(ValueError):
+            call()
+    p = [torch.zeros(4)]
+    for call in (lambda: lb.adamw(p, p, p, p, 1), lambda: lb.adamw(p, [], p, p, 1), lambda: lb.adamw(p, p, p, p, 1, first_scales=p),
+                 lambda: lb.adamw(p, p, p, p, 1, masters=[])):
+        with pytest.raises(ValueError):
+            call()
+    lb.adamw([], [], [], [], 1)
+
+
+def test_the_optimizer_refuses():
+    from paper_2506_22714_amd.optim import AdamW
+    p = [torch.nn.Parameter(torch.zeros(4))]
+    for kw in (dict(state_bits=16), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1.0), dict(lr=torch.tensor(1e-3))):
+        with pytest.raises(ValueError):
+            AdamW(p, **kw)
