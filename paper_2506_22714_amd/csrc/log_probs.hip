@@ -3,6 +3,9 @@
 //   log p_j = z_j - log s          H = log s - sum exp(z_j) z_j / s
 //   dx_j = scale * ([j = target] d + sum_a [j = top_a] d_a - p_j (d + sum_a d_a + e (log p_j + H)))
 // where d, d_a and e are the gradients of the target's, the alternatives' log probabilities and the entropy.
+//
+// The forward pass reads the logits once: maximum, s and sum exp(z) z run along and are rescaled where the maximum grows, and the best
+// logits are kept in the lanes of a wave.  The backward pass reads them once more and writes as much.  Both are bound by memory.
 #include <algorithm>
 #include <cmath>
 
@@ -12,128 +15,470 @@ using namespace libra;
 
 namespace {
 
-constexpr float INF = __builtin_inff();
+constexpr float INF = __builtin_inff(), LOWEST = -0x1.fffffep127f, LOG2E = 1.44269504088896340736f;
+constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 1024, MAX_PARTS = 64;
+static_assert(MAX_TOP <= WAVE_LANES, "a list of the best logits has a lane for each");
 
-// Whole numbers in the order of the logits, NaN last; a larger one comes first among the alternatives.  Zeros are equal.
+// NaN if one of them is
+__device__ inline float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// Whole numbers in the order of the logits, NaN last; a larger one comes first among the alternatives.  Zeros are equal.  Zero is no logit's.
 __device__ inline uint32_t rank_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return x != x ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ inline float logit_of(uint32_t rank) { return __uint_as_float(rank == 0xffffffffu ? 0x7fc00000u : rank & 0x80000000u ? rank ^ 0x80000000u : ~rank); }
 // ... and among equal ones the lower class
-__device__ inline uint64_t rank_of(float x, uint32_t j) { return (uint64_t)rank_of(x) << 32 | (0xffffffffu - j); }
-
-__device__ inline float wave_sum(float x) {
-    for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
-    return x;
+__device__ inline uint64_t key_of(float x, uint32_t j) { return (uint64_t)rank_of(x) << 32 | (0xffffffffu - j); }
+__device__ inline uint32_t class_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+__device__ inline uint64_t read_lane(uint64_t x, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
 }
-__device__ inline uint64_t wave_most(uint64_t x) {
-    for (int d = 32; d; d /= 2) {
-        const uint64_t y = __shfl_xor((unsigned long long)x, d);
-        x = x > y ? x : y;
+
+// Maximum, sum of exp(scale (x - maximum)) and sum of exp(scale (x - maximum)) (x - maximum) of some logits
+struct Sums {
+    float m = -INF, s = 0.f, t = 0.f;
+    // these sums with the maximum `m2`, which is not below m
+    __device__ void raise(float m2, float c) {
+        const float d = m == -INF ? 0.f : m - m2, f = m == -INF ? 0.f : __builtin_amdgcn_exp2f(d * c);
+        t = f == 0.f && s == s ? 0.f : f * (t + d * s);
+        s *= f;
+        m = m2;
     }
-    return x;
+    __device__ void join(Sums o, float c) {
+        const float m2 = larger(m, o.m);
+        raise(m2, c);
+        o.raise(m2, c);
+        s += o.s;
+        t += o.t;
+    }
+    // N more logits; what is no logit comes as -Inf.  c = scale * log2 e
+    template <int N> __device__ void add(const float *x, float most, float c) {
+        raise(larger(m, most), c);
+        const float base = m == -INF ? 0.f : m;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float d = x[k] - base, e = __builtin_amdgcn_exp2f(d * c);
+            s += e;
+            t = fmaf(e, fmaxf(d, LOWEST), t);       // 0 where the class is masked; NaN comes with e
+        }
+    }
+};
+
+template <int L> __device__ inline Sums over_group_sums(Sums a, float c) {
+    if constexpr (L > 1) {
+        const float m = over_group<L>(a.m, larger);
+        a.raise(m, c);
+        auto add = [](float x, float y) { return x + y; };
+        a.s = over_group<L>(a.s, add);
+        a.t = over_group<L>(a.t, add);
+    }
+    return a;
 }
 
-// a workgroup per row
-template <class T>
-__global__ __launch_bounds__(256) void log_probs_kernel(const T *logits, int64_t n, int64_t classes, int64_t ld, const void *targets, int index_type, int32_t top, float scale,
-                                                        float *target_out, float *entropy, float *top_out, int64_t *top_index, float *stats) {
-    __shared__ uint64_t best[4];
-    __shared__ float part[4][2];
+struct Forward {
+    int64_t n, classes, ld;
+    const void *targets;
+    int index_type;
+    int32_t top;
+    float scale;
+    float *target_out, *entropy, *top_out, *stats;
+    int64_t *top_index;
+};
+
+struct Finished {
+    float m, logs;
+    __device__ float logp(float x, float scale) const { return scale * (x - m) - logs; }
+};
+
+// What a row of -Inf has is 0 for the sums' sake: log p = -Inf - 0.
+__device__ inline Finished finish(const Sums &a) {
+    const bool empty = a.m == -INF;
+    return {empty ? 0.f : a.m, empty ? 0.f : logf(a.s)};
+}
+
+template <class T> __device__ inline void write_row(const Forward &f, const T *x, int64_t i, const Sums &a, const Finished &r) {
+    f.entropy[i] = a.m == -INF ? 0.f : r.logs - f.scale * (a.t / a.s);
+    f.stats[2 * i] = a.m;
+    f.stats[2 * i + 1] = r.logs;
+    if (f.targets) {
+        const int64_t j = index_at(f.targets, f.index_type, i);
+        f.target_out[i] = j >= 0 && j < f.classes ? r.logp(load_as_float(x[j]), f.scale) : j == -1 ? 0.f : __builtin_nanf("");
+    }
+}
+__device__ inline void write_alternative(const Forward &f, int64_t i, int a, uint64_t key, const Finished &r) {
+    f.top_out[i * f.top + a] = r.logp(logit_of((uint32_t)(key >> 32)), f.scale);
+    f.top_index[i * f.top + a] = class_of(key);
+}
+
+// ---- short rows: L lanes hold a row in registers, E logits each, in 16-byte pieces where every row is aligned to them ----
+template <class T, int L, int E> struct ShortRow {
+    static constexpr int W = VECTOR<T>, PIECES = E / W;
+    float x[E];
+    __device__ static int class_at(int lane, int e) { return (lane + L * (e / W)) * W + e % W; }
+    __device__ void load(const T *row, int classes, int lane, bool whole, bool there) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int j = class_at(lane, p * W);
+            if (whole && there && j + W <= classes) unpack<T>(*reinterpret_cast<const uint4 *>(row + j), x + p * W);
+            else {
+#pragma unroll
+                for (int k = 0; k < W; ++k) x[p * W + k] = there && j + k < classes ? load_as_float(row[j + k]) : -INF;
+            }
+        }
+    }
+};
+
+// The best logits one after another: the best of each lane's, then of the group's; the lane that has it drops it.
+template <class T, int L, int E> __device__ inline void short_alternatives(const Forward &f, const ShortRow<T, L, E> &row, int64_t i, int lane, bool there, const Finished &r) {
+    uint32_t rank[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) rank[e] = ShortRow<T, L, E>::class_at(lane, e) < f.classes ? rank_of(row.x[e]) : 0;
+    for (int a = 0; a < f.top; ++a) {
+        uint32_t best = rank[0];
+        int at = 0;
+#pragma unroll
+        for (int e = 1; e < E; ++e)
+            if (rank[e] > best) best = rank[e], at = e;     // classes ascend with e
+        const uint64_t mine = (uint64_t)best << 32 | (0xffffffffu - (uint32_t)ShortRow<T, L, E>::class_at(lane, at));
+        const uint64_t key = over_group<L>(mine, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
+        if (mine == key) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e == at) rank[e] = 0;
+        }
+        if (there && lane == a % L) write_alternative(f, i, a, key, r);
+    }
+}
+
+template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits, bool whole) {
+    const int lane = threadIdx.x % L;
+    const float c = f.scale * LOG2E;
+    constexpr int EACH = 256 / L;
+    for (int64_t base = (int64_t)blockIdx.x * EACH; base < f.n; base += (int64_t)gridDim.x * EACH) {
+        const int64_t i = base + threadIdx.x / L;
+        const bool there = i < f.n;
+        ShortRow<T, L, E> row;
+        row.load(logits + i * f.ld, (int)f.classes, lane, whole, there);
+        float most = row.x[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) most = larger(most, row.x[e]);
+        Sums a;
+        a.template add<E>(row.x, over_group<L>(most, larger), c);
+        auto add = [](float x, float y) { return x + y; };
+        a.s = over_group<L>(a.s, add);
+        a.t = over_group<L>(a.t, add);
+        const Finished r = finish(a);
+        if (there && lane == 0) write_row(f, logits + i * f.ld, i, a, r);
+        if (f.top) short_alternatives(f, row, i, lane, there, r);
+    }
+}
+
+// ---- long rows: a workgroup walks a row, or a part of it where there are few rows ----
+
+// The best logits that a wave has seen, in descending order, one in each of the first `top` lanes.
+struct Best {
+    uint64_t key = 0;               // this lane's
+    uint64_t limit = 0;             // the last one of the list; 0 while it is not full
+    // every lane brings a key, or 0
+    __device__ void insert(uint64_t brought, int top) {
+        for (;;) {
+            const uint64_t those = __ballot(brought > limit);
+            if (!those) return;
+            const int lane = 63 - __builtin_clzll(those);
+            const uint64_t x = read_lane(brought, lane);
+            if ((int)(threadIdx.x % WAVE_LANES) == lane) brought = 0;
+            // the list with x: b_k = max(a_k, min(a_(k-1), x))
+            const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)(uint32_t)(key >> 32), 0x138, 0xf, 0xf, false);    // wave_shr:1
+            const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)(uint32_t)key, 0x138, 0xf, 0xf, false);
+            const uint64_t above = (uint64_t)high << 32 | low, place = above < x ? above : x;
+            key = key > place ? key : place;
+            limit = read_lane(key, top - 1);
+        }
+    }
+    __device__ float threshold() const { return limit ? logit_of((uint32_t)(limit >> 32)) : -INF; }
+};
+
+// The `top` best of `lists` descending lists of `top` keys in LDS, by one wave: f(a, key), the same key in every lane.
+template <class F> __device__ inline void merge_lists(const uint64_t *keys, int lists, int top, F &&f) {
+    const int lane = threadIdx.x % WAVE_LANES;
+    int at = 0;
+    uint64_t head = lane < lists ? keys[lane * top] : 0;
+    for (int a = 0; a < top; ++a) {
+        const uint64_t best = over_group<WAVE_LANES>(head, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
+        if (head == best) {                             // keys differ, but for the zeros of lists that are not full
+            ++at;
+            head = lane < lists && at < top ? keys[lane * top + at] : 0;
+        }
+        f(a, best);
+    }
+}
+
+struct Parts {                      // of rows that several workgroups share
+    int32_t count;
+    float *sums;                    // 3 for each part of each row
+    uint64_t *keys;                 // top for each
+};
+
+constexpr int LONG_THREADS = 256, LONG_WAVES = LONG_THREADS / WAVE_LANES;
+
+template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_kernel(Forward f, const T *logits, Parts parts) {
+    constexpr int W = VECTOR<T>, U = 16 / W, N = U * W;
+    __shared__ float shared_sums[LONG_WAVES][3];
+    __shared__ uint64_t shared_keys[LONG_WAVES * MAX_TOP];
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const T *x = logits + i * ld;
-    // the largest logit that comes after `limit`
-    auto next = [&](uint64_t limit) {
-        uint64_t most = 0;
-        for (int64_t j = threadIdx.x; j < classes; j += 256) {
-            const uint64_t r = rank_of(load_as_float(x[j]), (uint32_t)j);
-            if (r < limit && r > most) most = r;
+    const float c = f.scale * LOG2E;
+    for (int64_t unit = blockIdx.x; unit < f.n * parts.count; unit += gridDim.x) {
+        const int64_t i = unit / parts.count;
+        const int part = (int)(unit % parts.count);
+        const T *x = logits + i * f.ld;
+        // 16-byte pieces of memory: the first and the last may hold other things beside the row
+        const int before = (int)((uintptr_t)x % 16 / sizeof(T));
+        const int64_t pieces = (before + f.classes + W - 1) / W, each = (pieces + parts.count - 1) / parts.count, begin = part * each, end = min(pieces, begin + each);
+        auto fetch = [&](int64_t v, uint4 *raw) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t p = v + u * LONG_THREADS, j = p * W - before;
+                if (p < end && j >= 0 && j + W <= f.classes) raw[u] = *reinterpret_cast<const uint4 *>(x + j);
+                else {
+                    float y[W];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) y[k] = p < end && j + k >= 0 && j + k < f.classes ? load_as_float(x[j + k]) : -INF;
+                    raw[u] = pack<T>(y);
+                }
+            }
+        };
+        Sums a;
+        Best best;
+        uint4 raw[U], next[U];
+        fetch(begin + threadIdx.x, raw);
+        for (int64_t v0 = begin; v0 < end; v0 += U * LONG_THREADS) {
+            const int64_t v = v0 + threadIdx.x;
+            fetch(v + U * LONG_THREADS, next);          // on its way while this one is worked on
+            float y[N];
+#pragma unroll
+            for (int u = 0; u < U; ++u) unpack<T>(raw[u], y + u * W);
+            float most = y[0];
+#pragma unroll
+            for (int k = 1; k < N; ++k) most = larger(most, y[k]);
+            a.template add<N>(y, most, c);
+            if (f.top) {
+                float limit = best.threshold();
+                if (__ballot(!(most < limit))) {        // rarely, once the list is full of large ones
+#pragma unroll
+                    for (int k = N - 1; k >= 0; --k) {
+                        const bool near = !(y[k] < limit);
+                        if (!__ballot(near)) continue;
+                        const int64_t p = v + (k / W) * LONG_THREADS, j = p * W + k % W - before;
+                        best.insert(near && p < end && j >= 0 && j < f.classes ? key_of(y[k], (uint32_t)j) : 0, f.top);
+                        limit = best.threshold();
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = next[u];
         }
-        most = wave_most(most);
+        a = over_group_sums<WAVE_LANES>(a, c);
+        if (lane == 0) shared_sums[wave][0] = a.m, shared_sums[wave][1] = a.s, shared_sums[wave][2] = a.t;
+        if (lane < f.top) shared_keys[wave * f.top + lane] = best.key;
         __syncthreads();
-        if (lane == 0) best[wave] = most;
+        if (wave == 0) {
+            a = Sums{};
+            for (int w = 0; w < LONG_WAVES; ++w) a.join(Sums{shared_sums[w][0], shared_sums[w][1], shared_sums[w][2]}, c);
+            if (parts.count == 1) {
+                const Finished r = finish(a);
+                if (lane == 0) write_row(f, x, i, a, r);
+                if (f.top) merge_lists(shared_keys, LONG_WAVES, f.top, [&](int k, uint64_t key) {
+                    if (lane == 0) write_alternative(f, i, k, key, r);
+                });
+            } else {
+                if (lane == 0) parts.sums[3 * unit] = a.m, parts.sums[3 * unit + 1] = a.s, parts.sums[3 * unit + 2] = a.t;
+                if (f.top) merge_lists(shared_keys, LONG_WAVES, f.top, [&](int k, uint64_t key) {
+                    if (lane == 0) parts.keys[unit * f.top + k] = key;
+                });
+            }
+        }
         __syncthreads();
-        for (int w = 0; w < 4; ++w) most = most > best[w] ? most : best[w];
-        return most;
-    };
-    uint64_t r = next(~0ull);
-    const float most = load_as_float(x[0xffffffffu - (uint32_t)r]);
-    const bool empty = most == -INF;
-    float s = 0.f, t = 0.f;
-    for (int64_t j = threadIdx.x; j < classes; j += 256) {
-        const float z = scale * (load_as_float(x[j]) - (empty ? 0.f : most)), e = expf(z);
-        s += e;
-        if (e != 0.f) t += e * z;
-    }
-    s = wave_sum(s);
-    t = wave_sum(t);
-    if (lane == 0) part[wave][0] = s, part[wave][1] = t;
-    __syncthreads();
-    s = t = 0.f;
-    for (int w = 0; w < 4; ++w) s += part[w][0], t += part[w][1];
-    const float logs = empty ? 0.f : logf(s);
-    auto logp = [&](int64_t j) { return scale * (load_as_float(x[j]) - (empty ? 0.f : most)) - logs; };
-    if (threadIdx.x == 0) {
-        entropy[i] = empty ? 0.f : logs - t / s;
-        stats[2 * i] = most;
-        stats[2 * i + 1] = logs;
-        if (targets) {
-            const int64_t j = index_at(targets, index_type, i);
-            target_out[i] = j >= 0 && j < classes ? logp(j) : j == -1 ? 0.f : __builtin_nanf("");
-        }
-    }
-    for (int32_t a = 0; a < top; ++a) {
-        const int64_t j = 0xffffffffu - (uint32_t)r;
-        if (threadIdx.x == 0) {
-            top_out[i * top + a] = logp(j);
-            top_index[i * top + a] = j;
-        }
-        if (a + 1 < top) r = next(r);
-    }
-    __syncthreads();
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void log_probs_backward_kernel(const T *logits, int64_t n, int64_t classes, int64_t ld, const void *targets, int index_type, int32_t top,
-                                                                 float scale, const float *entropy, const float *stats, const int64_t *top_index, const float *d_target,
-                                                                 const float *d_entropy, const float *d_top, T *dlogits, int64_t ld_dlogits) {
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const T *x = logits + i * ld;
-    const float most = stats[2 * i], logs = stats[2 * i + 1], h = entropy[i];
-    const int64_t target = targets ? index_at(targets, index_type, i) : -1;
-    const bool given = target >= 0 && target < classes;
-    const float e = d_entropy ? d_entropy[i] : 0.f;
-    const float d = target == -1 || !d_target ? 0.f : given ? d_target[i] : __builtin_nanf("");
-    float all = d;
-    if (d_top)
-        for (int a = 0; a < top; ++a) all += d_top[i * top + a];
-    for (int64_t j = threadIdx.x; j < classes; j += 256) {
-        const float logp = scale * (load_as_float(x[j]) - most) - logs, p = expf(logp);
-        float g = p == 0.f ? 0.f * all : -p * (all + e * (logp + h));
-        if (j == target) g += d;
-        if (d_top)
-            for (int a = 0; a < top; ++a)
-                if (top_index[i * top + a] == j) g += d_top[i * top + a];
-        dlogits[i * ld_dlogits + j] = round_to<T>(most == -INF ? 0.f : scale * g);
+// a workgroup joins the parts of a row
+template <class T> __global__ __launch_bounds__(256) void join_parts_kernel(Forward f, const T *logits, Parts parts) {
+    extern __shared__ uint64_t keys[];
+    const int lane = threadIdx.x % WAVE_LANES;
+    const float c = f.scale * LOG2E;
+    for (int64_t i = blockIdx.x; i < f.n; i += gridDim.x) {
+        for (int k = threadIdx.x; k < parts.count * f.top; k += 256) keys[k] = parts.keys[i * parts.count * f.top + k];
+        __syncthreads();
+        if (threadIdx.x < WAVE_LANES) {
+            Sums a;
+            if (lane < parts.count) {
+                const float *p = parts.sums + 3 * (i * parts.count + lane);
+                a = Sums{p[0], p[1], p[2]};
+            }
+            a = over_group_sums<WAVE_LANES>(a, c);
+            const Finished r = finish(a);
+            if (lane == 0) write_row(f, logits + i * f.ld, i, a, r);
+            if (f.top) merge_lists(keys, parts.count, f.top, [&](int k, uint64_t key) {
+                if (lane == 0) write_alternative(f, i, k, key, r);
+            });
+        }
+        __syncthreads();
     }
+}
+
+// ---- gradient ----
+struct Backward {
+    int64_t n, classes, ld, ld_out;
+    const void *targets;
+    int index_type;
+    int32_t top;
+    float scale;
+    const float *entropy, *stats, *d_target, *d_entropy, *d_top;
+    const int64_t *top_index;
+};
+
+// dx_j = p_j (a + b log p_j) plus what the target and the alternatives get on top; a = -scale (d + sum d_a + e H), b = -scale e
+struct RowGradient {
+    float m, logs, a, b, d;
+    int64_t target;
+    bool empty;
+    __device__ RowGradient(const Backward &g, int64_t i) {
+        m = g.stats[2 * i];
+        logs = g.stats[2 * i + 1];
+        empty = m == -INF;
+        target = g.targets ? index_at(g.targets, g.index_type, i) : -1;
+        d = target == -1 || !g.d_target ? 0.f : target >= 0 && target < g.classes ? g.d_target[i] : __builtin_nanf("");
+        float all = d;
+        if (g.d_top)
+            for (int k = 0; k < g.top; ++k) all += g.d_top[i * g.top + k];
+        const float e = g.d_entropy ? g.d_entropy[i] : 0.f;
+        a = -g.scale * fmaf(e, g.entropy[i], all);
+        b = -g.scale * e;
+    }
+    __device__ float at(float x, float scale) const {
+        const float logp = fmaf(scale, x - m, -logs), p = __builtin_amdgcn_exp2f(logp * LOG2E);
+        return empty ? 0.f : p * fmaf(b, fmaxf(logp, LOWEST), a);      // a masked class: p = 0; NaN comes with p
+    }
+};
+
+template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_backward_kernel(Backward g, const T *logits, T *out, bool whole) {
+    typedef ShortRow<T, L, E> Row;
+    const int lane = threadIdx.x % L;
+    constexpr int EACH = 256 / L;
+    for (int64_t base = (int64_t)blockIdx.x * EACH; base < g.n; base += (int64_t)gridDim.x * EACH) {
+        const int64_t i = base + threadIdx.x / L;
+        if (i >= g.n) return;
+        Row row;
+        row.load(logits + i * g.ld, (int)g.classes, lane, whole, true);
+        const RowGradient r(g, i);
+        T *o = out + i * g.ld_out;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            row.x[e] = r.at(row.x[e], g.scale);
+            if (Row::class_at(lane, e) == r.target && !r.empty) row.x[e] = fmaf(g.scale, r.d, row.x[e]);
+        }
+        if (g.d_top && !r.empty)
+            for (int k = 0; k < g.top; ++k) {
+                const int64_t j = g.top_index[i * g.top + k];
+                const float more = g.scale * g.d_top[i * g.top + k];
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (Row::class_at(lane, e) == j) row.x[e] += more;
+            }
+#pragma unroll
+        for (int p = 0; p < Row::PIECES; ++p) {
+            const int j = Row::class_at(lane, p * Row::W);
+            if (whole && j + Row::W <= g.classes) *reinterpret_cast<uint4 *>(o + j) = pack<T>(row.x + p * Row::W);
+            else {
+#pragma unroll
+                for (int k = 0; k < Row::W; ++k)
+                    if (j + k < g.classes) o[j + k] = round_to<T>(row.x[p * Row::W + k]);
+            }
+        }
+    }
+}
+
+// A workgroup takes a run of pieces of a row; the few classes that get more than p_j (...) are written a second time, whole.  Rows are
+// taken from the last to the first: the forward pass has just read the last ones.
+template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
+    constexpr int W = VECTOR<T>, U = 32 / W;
+    for (int64_t unit = (int64_t)blockIdx.x; unit < g.n * runs; unit += gridDim.x) {
+        const int64_t i = g.n - 1 - unit / runs, run = unit % runs;
+        const T *x = logits + i * g.ld;
+        T *o = out + i * g.ld_out;
+        const RowGradient r(g, i);
+        const int before = (int)((uintptr_t)x % 16 / sizeof(T));
+        const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
+        const int64_t first = run * (U * LONG_THREADS);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t j = (first + u * LONG_THREADS + threadIdx.x) * W - before;
+            float y[W];
+            if (alike && j >= 0 && j + W <= g.classes) {
+                unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
+#pragma unroll
+                for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
+                *reinterpret_cast<uint4 *>(o + j) = pack<T>(y);
+            } else {
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    if (j + k >= 0 && j + k < g.classes) o[j + k] = round_to<T>(r.at(load_as_float(x[j + k]), g.scale));
+            }
+        }
+        if (r.empty || (r.target < 0 && !g.d_top)) continue;        // the same for the whole workgroup
+        __syncthreads();
+        const int64_t low = first * W - before, high = low + (int64_t)U * LONG_THREADS * W;
+        const int k = threadIdx.x;
+        if (k <= (g.d_top ? g.top : 0)) {
+            const int64_t j = k ? g.top_index[i * g.top + k - 1] : r.target;
+            if (j >= 0 && j >= low && j < high && j < g.classes) {
+                float more = j == r.target ? r.d : 0.f;
+                if (g.d_top)
+                    for (int a = 0; a < g.top; ++a)
+                        if (g.top_index[i * g.top + a] == j) more += g.d_top[i * g.top + a];
+                o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
+            }
+        }
+        __syncthreads();
     }
 }
 
 int shape(int64_t n, int64_t classes, int32_t top) {
     if (n < 0 || classes < 1 || top < 0 || top > classes) return LIBRA_ERR_SHAPE;
     if (n > INT32_MAX || classes > INT32_MAX) return LIBRA_ERR_TOO_LARGE;
-    if (top > LIBRA_LOG_PROBS_MAX_TOP) return LIBRA_ERR_UNSUPPORTED;
+    if (top > MAX_TOP) return LIBRA_ERR_UNSUPPORTED;
     return LIBRA_OK;
 }
+
+// Workgroups of long rows, and of each of them parts: enough to have several workgroups on every compute unit, each with a round of loads at least.
+int32_t part_count(int64_t n, int64_t classes) {
+    if (classes <= SHORT_CLASSES) return 1;
+    const int64_t wanted = (2048 + n - 1) / n, most = (classes + 4095) / 4096;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(wanted, most), MAX_PARTS));
+}
+
+size_t part_bytes(int64_t n, int32_t count, int32_t top) { return count == 1 ? 0 : ((size_t)n * count * 12 + 255) / 256 * 256 + (size_t)n * count * top * 8; }
+
+// f(lanes of a row, logits of a lane)
+template <class F> int for_short(int64_t classes, F &&f) {
+    typedef std::integral_constant<int, 8> E8;
+    typedef std::integral_constant<int, 16> E16;
+    if (classes <= 64) return f(std::integral_constant<int, 8>{}, E8{});
+    if (classes <= 128) return f(std::integral_constant<int, 16>{}, E8{});
+    if (classes <= 256) return f(std::integral_constant<int, 32>{}, E8{});
+    if (classes <= 512) return f(std::integral_constant<int, 64>{}, E8{});
+    return f(std::integral_constant<int, 64>{}, E16{});
+}
+
+constexpr int64_t MOST_WORKGROUPS = 1 << 23;        // the threads of a launch are counted in 32 bits
 
 }  // namespace
 
 extern "C" int libra_log_probs_workspace(int64_t n, int64_t classes, int32_t top, size_t *bytes) {
     if (!bytes) return LIBRA_ERR_NULL;
     if (int rc = shape(n, classes, top)) return rc;
-    *bytes = 0;
+    *bytes = n ? part_bytes(n, part_count(n, classes), top) : 0;
     return LIBRA_OK;
 }
 
@@ -148,10 +493,28 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
     if (!aligned_to(logits, dtype_bytes(dtype)) || (targets && !aligned_to(targets, index_bytes(index_type))) || !aligned_to(target_out, 4) || !aligned_to(entropy, 4) ||
         !aligned_to(top_out, 4) || !aligned_to(top_index, 8) || !aligned_to(stats, 4))
         return LIBRA_ERR_BUFFER;
+    Parts parts{part_count(n, classes), nullptr, nullptr};
+    if (const size_t need = part_bytes(n, parts.count, top)) {
+        if (!workspace) return LIBRA_ERR_NULL;
+        if (workspace_bytes < need || !aligned_to(workspace, 256)) return LIBRA_ERR_BUFFER;
+        parts.sums = (float *)workspace;
+        parts.keys = (uint64_t *)((char *)workspace + ((size_t)n * parts.count * 12 + 255) / 256 * 256);
+    }
+    const Forward f{n, classes, ld, targets, index_type, top, scale, target_out, entropy, top_out, stats, top_index};
+    hipStream_t s = (hipStream_t)stream;
     return for_dtype(dtype, [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((log_probs_kernel<T>), dim3((unsigned)std::min<int64_t>(n, 1 << 20)), dim3(256), 0, (hipStream_t)stream, (const T *)logits, n, classes, ld, targets, index_type, top, scale,
-                           target_out, entropy, top_out, top_index, stats);
+        const T *x = (const T *)logits;
+        if (classes <= SHORT_CLASSES) return for_short(classes, [&](auto lanes, auto each) {
+            constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
+            const bool whole = aligned_to(x, 16) && ld % VECTOR<T> == 0;
+            const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
+            hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x, whole);
+            return last_launch();
+        });
+        hipLaunchKernelGGL((long_rows_kernel<T>), dim3((unsigned)std::min<int64_t>(n * parts.count, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
+        if (parts.count > 1)
+            hipLaunchKernelGGL((join_parts_kernel<T>), dim3((unsigned)std::min<int64_t>(n, MOST_WORKGROUPS)), dim3(256), (size_t)parts.count * top * 8, s, f, x, parts);
         return last_launch();
     });
 }
@@ -168,10 +531,21 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
     if (!aligned_to(logits, dtype_bytes(dtype)) || !aligned_to(dlogits, dtype_bytes(dtype)) || (targets && !aligned_to(targets, index_bytes(index_type))) ||
         !aligned_to(entropy, 4) || !aligned_to(stats, 4) || !aligned_to(top_index, 8) || !aligned_to(d_target, 4) || !aligned_to(d_entropy, 4) || !aligned_to(d_top, 4))
         return LIBRA_ERR_BUFFER;
+    const Backward g{n, classes, ld, ld_dlogits, targets, index_type, top, scale, entropy, stats, d_target, d_entropy, top ? d_top : nullptr, top_index};
+    hipStream_t s = (hipStream_t)stream;
     return for_dtype(dtype, [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((log_probs_backward_kernel<T>), dim3((unsigned)std::min<int64_t>(n, 1 << 20)), dim3(256), 0, (hipStream_t)stream, (const T *)logits, n, classes, ld, targets, index_type, top,
-                           scale, entropy, stats, top_index, d_target, d_entropy, top ? d_top : nullptr, (T *)dlogits, ld_dlogits);
+        const T *x = (const T *)logits;
+        T *o = (T *)dlogits;
+        if (classes <= SHORT_CLASSES) return for_short(classes, [&](auto lanes, auto each) {
+            constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
+            const bool whole = aligned_to(x, 16) && ld % VECTOR<T> == 0 && aligned_to(o, 16) && ld_dlogits % VECTOR<T> == 0;
+            const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
+            hipLaunchKernelGGL((short_rows_backward_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, g, x, o, whole);
+            return last_launch();
+        });
+        const int64_t pieces = (classes + 2 * VECTOR<T> - 2) / VECTOR<T>, run = 32 / VECTOR<T> * LONG_THREADS, runs = (pieces + run - 1) / run;
+        hipLaunchKernelGGL((long_rows_backward_kernel<T>), dim3((unsigned)std::min<int64_t>(n * runs, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, g, x, o, (int32_t)runs);
         return last_launch();
     });
 }
