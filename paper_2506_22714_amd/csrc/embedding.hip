@@ -1,5 +1,6 @@
 // Rows of a learned table, scaled, and the gradient of the table.
 //   out[i] = scale * table[index[i]]            dtable[v] = scale * sum over i with index[i] = v of dout[i]
+// Both are bound by memory.
 #include <algorithm>
 
 #include "ends.h"
@@ -8,169 +9,537 @@ using namespace libra;
 
 namespace {
 
-template <class T>
+// Lanes that share a row: a power of two, 16 bytes each where the rows are aligned to them, an element each otherwise.
+template <class T, bool WHOLE> struct Piece {
+    static constexpr int W = WHOLE ? VECTOR<T> : 1;
+    float x[W];
+    __device__ void load(const T *p) {
+        if constexpr (WHOLE) unpack<T>(*reinterpret_cast<const uint4 *>(p), x);
+        else x[0] = load_as_float(p[0]);
+    }
+    __device__ void store(T *p) const {
+        if constexpr (WHOLE) *reinterpret_cast<uint4 *>(p) = pack<T>(x);
+        else p[0] = round_to<T>(x[0]);
+    }
+    __device__ void fill(float v) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) x[k] = v;
+    }
+    __device__ void scale(float s) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) x[k] *= s;
+    }
+    __device__ void add(const Piece &o) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) x[k] += o.x[k];
+    }
+};
+
+// ---- lookup: LOOKUP_ROWS rows of each group of lanes in flight ----
+constexpr int LOOKUP_ROWS = 4;
+
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(256) void embedding_kernel(const T *table, int64_t rows, int32_t width, int64_t ld_table, const void *index, int index_type, int64_t n,
-                                                        float scale, T *out, int64_t ld_out) {
-    const int lane = threadIdx.x % WAVE_LANES;
-    for (int64_t i = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE_LANES; i < n; i += (int64_t)gridDim.x * 4) {
-        const int64_t v = index_at(index, index_type, i);
-        const bool known = v >= 0 && v < rows;
-        const float other = v == -1 ? 0.f : __builtin_nanf("");
-        for (int32_t c = lane; c < width; c += WAVE_LANES)
-            out[i * ld_out + c] = round_to<T>(known ? scale * load_as_float(table[v * ld_table + c]) : other);
+                                                        float scale, T *out, int64_t ld_out, int lanes) {
+    typedef Piece<T, WHOLE> P;
+    const int groups = 256 / lanes, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
+    const int32_t pieces = width / P::W;
+    for (int64_t first = (int64_t)blockIdx.x * (groups * LOOKUP_ROWS); first < n; first += (int64_t)gridDim.x * (groups * LOOKUP_ROWS)) {
+        int64_t v[LOOKUP_ROWS];
+#pragma unroll
+        for (int u = 0; u < LOOKUP_ROWS; ++u) v[u] = index_at(index, index_type, min(first + u * groups + group, n - 1));
+        for (int32_t c = lane; c < pieces; c += lanes) {
+            P p[LOOKUP_ROWS];
+#pragma unroll
+            for (int u = 0; u < LOOKUP_ROWS; ++u) {
+                if (v[u] >= 0 && v[u] < rows) {
+                    p[u].load(table + v[u] * ld_table + c * P::W);
+                    p[u].scale(scale);
+                } else p[u].fill(v[u] == -1 ? 0.f : __builtin_nanf(""));
+            }
+#pragma unroll
+            for (int u = 0; u < LOOKUP_ROWS; ++u)
+                if (first + u * groups + group < n) p[u].store(out + (first + u * groups + group) * ld_out + c * P::W);
+        }
     }
 }
 
-// ---- sorting (key, place) pairs by key, eight bits at a time; equal keys keep their order ----
-constexpr int DIGITS = 256, SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / WAVE_LANES, SORT_BATCHES = 16, SORT_TILE = SORT_THREADS * SORT_BATCHES, SORT_BLOCKS = 64;
+// ---- gradient ----
+// Few ids: every workgroup owns a run of the table's rows.  It reads all ids, keeps those of its rows in LDS, brings them into the order
+// of their rows, adds the rows of dout up and writes its rows of the table, zeros among them: one launch, no array between.
+// Many ids: (row, place) pairs are sorted by row, the pairs are cut into runs of equal length whatever rows they name, the sums of rows
+// that a run holds whole are written, those of rows that go on beyond a run are joined by another launch.  The zeros are written
+// while the first pass of the sort, which is bound by latency, runs.
+
+__device__ inline uint32_t key_at(const void *index, int index_type, int64_t rows, int64_t i) {
+    const int64_t v = index_at(index, index_type, i);
+    return v >= 0 && v < rows ? (uint32_t)v : (uint32_t)rows;           // what is no row comes last
+}
+
+// Which lanes of the wave hold this lane's digit (0 for a lane without one)
+__device__ inline uint64_t same_digit(uint32_t digit, int bits, bool real) {
+    uint64_t same = __ballot(real);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    return real ? same : 0;
+}
+// Number of this digit in the wave so far (counted in LDS, where only this wave counts), among earlier batches and lower lanes
+__device__ inline int32_t rank_in_wave(uint32_t digit, int bits, bool real, int32_t *count) {
+    const int lane = threadIdx.x % WAVE_LANES;
+    const uint64_t same = same_digit(digit, bits, real);
+    const int before = __popcll(same & ((1ull << lane) - 1));
+    int32_t base = 0;
+    if (real && before == 0) base = atomicAdd(&count[digit], (int32_t)__popcll(same));
+    return __shfl(base, real ? __ffsll((unsigned long long)same) - 1 : 0) + before;
+}
+
+// -- few ids --
+constexpr int OWNER_THREADS = 1024, OWNER_WAVES = OWNER_THREADS / WAVE_LANES, OWNER_IDS = 16, OWNER_PLACE_BITS = 14, OWNER_MAX_IDS = 1 << OWNER_PLACE_BITS;
+constexpr int OWNER_ROW_BITS = 9, OWNER_ROWS = 1 << OWNER_ROW_BITS, OWNER_LONG = 32;    // rows with more ids than that are added up by the whole workgroup
+static_assert(OWNER_THREADS * OWNER_IDS == OWNER_MAX_IDS, "a thread holds its share of a full list");
+
+template <class T, bool WHOLE, int MOST>
+__global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int64_t ld_dout, const void *index, int index_type, int32_t n, int64_t rows, int32_t width,
+                                                              int32_t owned, float scale, T *dtable, int64_t ld_dtable, int lanes) {
+    typedef Piece<T, WHOLE> P;
+    __shared__ uint32_t list[MOST];                             // row in this run << OWNER_PLACE_BITS | place, n at most
+    __shared__ int32_t start[OWNER_ROWS], total[OWNER_WAVES], long_rows[OWNER_MAX_IDS / OWNER_LONG], longs;
+    __shared__ union {                                          // first the one, then the other
+        int32_t count[OWNER_WAVES][OWNER_ROWS];
+        float part[OWNER_THREADS * 8];
+    } shared;
+    int32_t(&count)[OWNER_WAVES][OWNER_ROWS] = shared.count;
+    float(&part)[OWNER_THREADS * 8] = shared.part;
+    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
+    const int64_t low = (int64_t)blockIdx.x * owned;
+    const int32_t mine = (int32_t)min((int64_t)owned, rows - low);
+
+    // the ids of these rows, in the order of their places
+    int32_t m = 0;
+    {
+        const int32_t each = (n + OWNER_THREADS - 1) / OWNER_THREADS;
+        uint32_t row[OWNER_IDS];
+        int32_t found = 0;
+#pragma unroll
+        for (int b = 0; b < OWNER_IDS; ++b) {
+            const int32_t i = (wave * each + b) * WAVE_LANES + lane;
+            const int64_t v = b < each && i < n ? index_at(index, index_type, i) - low : -1;
+            row[b] = v >= 0 && v < mine ? (uint32_t)v : ~0u;
+        }
+#pragma unroll
+        for (int b = 0; b < OWNER_IDS; ++b) found += __popcll(__ballot(row[b] != ~0u));
+        if (lane == 0) total[wave] = found;
+        __syncthreads();
+        int32_t to = 0;
+        for (int w = 0; w < OWNER_WAVES; ++w) {
+            const int32_t t = total[w];
+            to += w < wave ? t : 0;
+            m += t;
+        }
+#pragma unroll
+        for (int b = 0; b < OWNER_IDS; ++b) {
+            const uint64_t those = __ballot(row[b] != ~0u);
+            if (row[b] != ~0u) list[to + __popcll(those & ((1ull << lane) - 1))] = row[b] << OWNER_PLACE_BITS | (uint32_t)((wave * each + b) * WAVE_LANES + lane);
+            to += __popcll(those);
+        }
+    }
+    for (int r = threadIdx.x; r < OWNER_WAVES * OWNER_ROWS; r += OWNER_THREADS) (&count[0][0])[r] = 0;
+    if (threadIdx.x == 0) longs = 0;
+    __syncthreads();
+
+    // into the order of their rows (`start`: where a row's ids begin)
+    {
+        const int32_t each = (m + OWNER_THREADS - 1) / OWNER_THREADS;
+        uint32_t item[OWNER_IDS];
+        int32_t rank[OWNER_IDS];
+#pragma unroll
+        for (int b = 0; b < OWNER_IDS; ++b) {
+            if (b < each) {
+                const int32_t q = (wave * each + b) * WAVE_LANES + lane;
+                item[b] = q < m ? list[q] : 0;
+                rank[b] = rank_in_wave(item[b] >> OWNER_PLACE_BITS, OWNER_ROW_BITS, q < m, count[wave]);
+            }
+        }
+        __syncthreads();
+        // a row's number over all waves, then the sum of the rows before: OWNER_ROWS threads
+        int32_t sum = 0;
+        if (threadIdx.x < OWNER_ROWS)
+            for (int w = 0; w < OWNER_WAVES; ++w) {
+                const int32_t c = count[w][threadIdx.x];
+                count[w][threadIdx.x] = sum;
+                sum += c;
+            }
+        int32_t up_to = sum;
+        for (int d = 1; d < WAVE_LANES; d *= 2) {
+            const int32_t y = __shfl_up(up_to, d);
+            if (lane >= d) up_to += y;
+        }
+        if (lane == WAVE_LANES - 1) total[wave] = up_to;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) up_to += total[w];
+        if (threadIdx.x < OWNER_ROWS) start[threadIdx.x] = up_to - sum;
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < OWNER_IDS; ++b) {
+            const int32_t q = (wave * each + b) * WAVE_LANES + lane;
+            if (b < each && q < m) {
+                const int32_t r = item[b] >> OWNER_PLACE_BITS;
+                list[start[r] + count[wave][r] + rank[b]] = item[b];
+            }
+        }
+        __syncthreads();
+    }
+
+    const int groups = OWNER_THREADS / lanes, group = threadIdx.x / lanes;
+    const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;        // this lane's columns
+    const bool there = c < width;
+    auto end_of = [&](int32_t r) { return r + 1 < OWNER_ROWS ? start[r + 1] : m; };
+    auto sum_of = [&](int32_t q, int32_t end, P &sum) {                          // four rows in flight
+        for (; q < end; q += 4) {
+            P p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (q + u < end) p[u].load(dout + (int64_t)(list[q + u] & (OWNER_MAX_IDS - 1)) * ld_dout + c);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (q + u < end) sum.add(p[u]);
+        }
+    };
+    for (int32_t r = group; r < mine; r += groups) {
+        const int32_t begin = start[r], end = end_of(r);
+        if (end - begin > OWNER_LONG) {
+            if (threadIdx.x % lanes == 0) long_rows[atomicAdd(&longs, 1)] = r;
+            continue;
+        }
+        if (!there) continue;
+        P sum;
+        sum.fill(0.f);
+        sum_of(begin, end, sum);
+        sum.scale(scale);
+        sum.store(dtable + (low + r) * ld_dtable + c);
+    }
+    __syncthreads();
+    const int32_t all = longs;
+    for (int32_t k = 0; k < all; ++k) {
+        const int32_t r = long_rows[k], begin = start[r], end = end_of(r), each = (end - begin + groups - 1) / groups;
+        P sum;
+        sum.fill(0.f);
+        if (there) sum_of(begin + group * each, min(end, begin + (group + 1) * each), sum);
+#pragma unroll
+        for (int w = 0; w < P::W; ++w) part[w * OWNER_THREADS + threadIdx.x] = sum.x[w];
+        __syncthreads();
+        if (group == 0 && there) {
+            for (int g = 1; g < groups; ++g)
+#pragma unroll
+                for (int w = 0; w < P::W; ++w) sum.x[w] += part[w * OWNER_THREADS + g * lanes + threadIdx.x];
+            sum.scale(scale);
+            sum.store(dtable + (low + r) * ld_dtable + c);
+        }
+        __syncthreads();
+    }
+}
+
+// -- many ids: pairs sorted by row, up to 11 bits at a time; equal rows keep the order of their places --
+constexpr int DIGIT_BITS = 11, DIGITS = 1 << DIGIT_BITS, SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / WAVE_LANES, SORT_BATCHES = 16;
+constexpr int SORT_TILE = SORT_THREADS * SORT_BATCHES, SORT_BLOCKS = 512, SCAN_DIGITS = WAVE_LANES;
 
 struct Keys {                       // of one pass: the ids themselves in the first one, pairs afterwards
     const void *index;
     int index_type;
     int64_t rows;
-    const uint32_t *key;
-    const int32_t *place;
-    __device__ uint32_t at(int64_t i) const {
-        if (key) return key[i];
-        const int64_t v = index_at(index, index_type, i);
-        return v >= 0 && v < rows ? (uint32_t)v : (uint32_t)rows;       // what is no row comes last
-    }
-    __device__ int32_t place_of(int64_t i) const { return key ? place[i] : (int32_t)i; }
+    const uint2 *pair;
+    __device__ uint2 at(int64_t i) const { return pair ? pair[i] : uint2{key_at(index, index_type, rows, i), (uint32_t)i}; }
 };
 
-__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Keys in, int64_t n, int64_t each, int shift, int32_t *count) {
+// What the zeros of the table are written to by the launch of the first count: workgroups behind the counting ones
+struct Zeros {
+    char *base;
+    int64_t rows, width_bytes, ld_bytes;
+    unsigned blocks;
+};
+__device__ inline void write_zeros(const Zeros &z, unsigned block) {
+    const int64_t first = (int64_t)block * SORT_THREADS + threadIdx.x, step = (int64_t)z.blocks * SORT_THREADS;
+    if (z.width_bytes == z.ld_bytes && ((uintptr_t)z.base & 15) == 0) {
+        const int64_t bytes = z.rows * z.width_bytes;
+        uint4 *p = reinterpret_cast<uint4 *>(z.base);
+        for (int64_t k = first; k < bytes / 16; k += step) p[k] = uint4{0, 0, 0, 0};
+        if (first < bytes % 16) z.base[bytes / 16 * 16 + first] = 0;
+        return;
+    }
+    const int64_t halves = z.width_bytes / 2;               // a wave per row
+    for (int64_t r = first / WAVE_LANES; r < z.rows; r += step / WAVE_LANES)
+        for (int64_t k = threadIdx.x % WAVE_LANES; k < halves; k += WAVE_LANES) reinterpret_cast<uint16_t *>(z.base + r * z.ld_bytes)[k] = 0;
+}
+
+// count[block][digit]
+__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, unsigned blocks, int32_t *count, Zeros zeros) {
     __shared__ int32_t seen[DIGITS];
-    seen[threadIdx.x] = 0;
+    if (blockIdx.x >= blocks) {
+        write_zeros(zeros, blockIdx.x - blocks);
+        return;
+    }
+    for (int d = threadIdx.x; d < DIGITS; d += SORT_THREADS) seen[d] = 0;
     __syncthreads();
     const int64_t begin = (int64_t)blockIdx.x * each, end = min(n, begin + each);
-    for (int64_t i = begin + threadIdx.x; i < end; i += SORT_THREADS) atomicAdd(&seen[(in.at(i) >> shift) & (DIGITS - 1)], 1);
+    for (int64_t i = begin + threadIdx.x; i < end; i += 8 * SORT_THREADS) {
+        uint32_t key[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) key[u] = in.at(min(i + u * SORT_THREADS, end - 1)).x;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u * SORT_THREADS < end) atomicAdd(&seen[(key[u] >> shift) & ((1u << bits) - 1)], 1);
+    }
     __syncthreads();
-    count[threadIdx.x * gridDim.x + blockIdx.x] = seen[threadIdx.x];
+    for (int d = threadIdx.x; d < 1 << bits; d += SORT_THREADS) count[(int64_t)blockIdx.x * DIGITS + d] = seen[d];
 }
 
-// exclusive prefix sums of n counts, one workgroup
-__global__ __launch_bounds__(1024) void sort_scan_kernel(int32_t *count, int n) {
-    __shared__ int32_t part[1024];
-    const int each = (n + 1023) / 1024, begin = min(n, (int)threadIdx.x * each), end = min(n, begin + each);
-    int32_t sum = 0;
-    for (int i = begin; i < end; ++i) sum += count[i];
-    part[threadIdx.x] = sum;
+// For 64 digits: number of the digit in earlier blocks in place of the counts, and the digit's total.  Sixteen waves share the blocks.
+__global__ __launch_bounds__(1024) void sort_scan_kernel(int32_t *count, int blocks, int32_t *totals) {
+    __shared__ int32_t part[16][WAVE_LANES];
+    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES, each = (blocks + 15) / 16;
+    const int digit = blockIdx.x * SCAN_DIGITS + lane, begin = min(blocks, wave * each), end = min(blocks, begin + each);
+    constexpr int MOST = SORT_BLOCKS / 16;
+    int32_t c[MOST], sum = 0;
+#pragma unroll
+    for (int b = 0; b < MOST; ++b) c[b] = begin + b < end ? count[(int64_t)(begin + b) * DIGITS + digit] : 0;
+#pragma unroll
+    for (int b = 0; b < MOST; ++b) sum += c[b];
+    part[wave][lane] = sum;
     __syncthreads();
-    for (int d = 1; d < 1024; d *= 2) {
-        const int32_t before = (int)threadIdx.x >= d ? part[threadIdx.x - d] : 0;
-        __syncthreads();
-        part[threadIdx.x] += before;
-        __syncthreads();
+    int32_t before = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        before += w < wave ? part[w][lane] : 0;
+        all += part[w][lane];
     }
-    sum = part[threadIdx.x] - sum;
-    for (int i = begin; i < end; ++i) {
-        const int32_t c = count[i];
-        count[i] = sum;
-        sum += c;
+    if (wave == 0) totals[digit] = all;
+#pragma unroll
+    for (int b = 0; b < MOST; ++b) {
+        if (begin + b < end) count[(int64_t)(begin + b) * DIGITS + digit] = before;
+        before += c[b];
     }
 }
 
-__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, const int32_t *first, uint32_t *key_out, int32_t *place_out) {
-    __shared__ int32_t next[DIGITS], mine[SORT_WAVES][DIGITS];
-    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
-    next[threadIdx.x] = first[threadIdx.x * gridDim.x + blockIdx.x];
+__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, const int32_t *count, const int32_t *totals, uint2 *out) {
+    __shared__ int32_t next[DIGITS], mine[SORT_WAVES][DIGITS], part[SORT_WAVES];
+    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES, digits = 1 << bits;
+    {   // where this block's first pair of each digit goes: totals of the digits before, and what earlier blocks have
+        constexpr int EACH = DIGITS / SORT_THREADS;
+        int32_t t[EACH], sum = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int d = threadIdx.x * EACH + k;
+            t[k] = d < digits ? totals[d] : 0;
+            sum += t[k];
+        }
+        int32_t up_to = sum;
+        for (int d = 1; d < WAVE_LANES; d *= 2) {
+            const int32_t y = __shfl_up(up_to, d);
+            if (lane >= d) up_to += y;
+        }
+        if (lane == WAVE_LANES - 1) part[wave] = up_to;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) up_to += part[w];
+        up_to -= sum;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int d = threadIdx.x * EACH + k;
+            next[d] = d < digits ? up_to + count[(int64_t)blockIdx.x * DIGITS + d] : 0;
+            up_to += t[k];
+        }
+    }
     const int64_t begin = (int64_t)blockIdx.x * each, end = min(n, begin + each);
     for (int64_t tile = begin; tile < end; tile += SORT_TILE) {
-        for (int w = 0; w < SORT_WAVES; ++w) mine[w][threadIdx.x] = 0;
+        for (int d = threadIdx.x; d < SORT_WAVES * DIGITS; d += SORT_THREADS) (&mine[0][0])[d] = 0;
         __syncthreads();
-        uint32_t key[SORT_BATCHES];
+        uint2 pair[SORT_BATCHES];
         int32_t rank[SORT_BATCHES];
         const int64_t at = tile + (int64_t)wave * (SORT_BATCHES * WAVE_LANES) + lane;
 #pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b) key[b] = at + b * WAVE_LANES < end ? in.at(at + b * WAVE_LANES) : 0;
+        for (int b = 0; b < SORT_BATCHES; ++b) pair[b] = in.at(min(at + b * WAVE_LANES, end - 1));
 #pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b) {
-            const bool real = at + b * WAVE_LANES < end;
-            const uint32_t digit = (key[b] >> shift) & (DIGITS - 1);
-            uint64_t same = __ballot(real);             // lanes with this lane's digit
-#pragma unroll
-            for (int bit = 0; bit < 8; ++bit) {
-                const uint64_t set = __ballot((digit >> bit) & 1);
-                same &= (digit >> bit) & 1 ? set : ~set;
+        for (int b = 0; b < SORT_BATCHES; ++b) rank[b] = rank_in_wave((pair[b].x >> shift) & (digits - 1), bits, at + b * WAVE_LANES < end, mine[wave]);
+        __syncthreads();
+        for (int d = threadIdx.x; d < digits; d += SORT_THREADS) {
+            int32_t place = next[d];
+            for (int w = 0; w < SORT_WAVES; ++w) {
+                const int32_t c = mine[w][d];
+                mine[w][d] = place;
+                place += c;
             }
-            const int before = __popcll(same & ((1ull << lane) - 1));
-            int32_t base = 0;
-            if (real && before == 0) base = atomicAdd(&mine[wave][digit], (int32_t)__popcll(same));
-            rank[b] = __shfl(base, real ? __ffsll((unsigned long long)same) - 1 : 0) + before;
+            next[d] = place;
         }
-        __syncthreads();
-        int32_t place = next[threadIdx.x];
-        for (int w = 0; w < SORT_WAVES; ++w) {
-            const int32_t c = mine[w][threadIdx.x];
-            mine[w][threadIdx.x] = place;
-            place += c;
-        }
-        next[threadIdx.x] = place;
         __syncthreads();
 #pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b) {
-            const int64_t i = at + b * WAVE_LANES;
-            if (i >= end) continue;
-            const int32_t to = mine[wave][(key[b] >> shift) & (DIGITS - 1)] + rank[b];
-            key_out[to] = key[b];
-            place_out[to] = in.place_of(i);
-        }
+        for (int b = 0; b < SORT_BATCHES; ++b)
+            if (at + b * WAVE_LANES < end) out[mine[wave][(pair[b].x >> shift) & (digits - 1)] + rank[b]] = pair[b];
         __syncthreads();
     }
 }
 
-// first of n sorted keys that is not below `v`
-__device__ inline int64_t first_not_below(const uint32_t *key, int64_t n, uint32_t v) {
-    int64_t low = 0, high = n;
-    while (low < high) {
-        const int64_t mid = (low + high) / 2;
-        if (key[mid] < v) low = mid + 1;
-        else high = mid;
-    }
-    return low;
-}
-
-// a wave per row of the table
-template <class T>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(const T *dout, int64_t ld_dout, const uint32_t *key, const int32_t *place, int64_t n, int64_t rows, int32_t width,
-                                                            float scale, T *dtable, int64_t ld_dtable) {
-    const int lane = threadIdx.x % WAVE_LANES;
-    for (int64_t v = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE_LANES; v < rows; v += (int64_t)gridDim.x * 4) {
-        const int64_t begin = first_not_below(key, n, (uint32_t)v), end = first_not_below(key, n, (uint32_t)v + 1);
-        for (int32_t c = lane; c < width; c += WAVE_LANES) {
-            float sum = 0.f;
-            for (int64_t q = begin; q < end; q += 8) {
-                float x[8];
+// Runs of `run` pairs, a group of lanes each.  The row that a run begins in the middle of, and the one that goes on behind it, leave their
+// sums in `part` (two rows of fp32 for each run); a row that fills the whole run and goes on at both ends leaves the first of them.
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld_dout, const uint2 *pair, int64_t n, int32_t run, int64_t rows, int32_t width, float scale,
+                                                       T *dtable, int64_t ld_dtable, float *part, int32_t part_width, int lanes) {
+    typedef Piece<T, WHOLE> P;
+    constexpr int U = 8;
+    const int64_t k = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes, begin = k * run, end = min(n, begin + run);
+    const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;
+    if (begin >= n || c >= width) return;
+    uint32_t row = pair[begin].x;
+    bool whole = begin == 0 || pair[begin - 1].x != row;            // the current row began here
+    P sum;
+    sum.fill(0.f);
+    auto leave = [&](bool ends) {
+        if (row >= (uint32_t)rows) return;
+        if (whole && ends) {
+            sum.scale(scale);
+            sum.store(dtable + (int64_t)row * ld_dtable + c);
+        } else {
+            float *to = part + (2 * k + (whole ? 1 : 0)) * part_width + c;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = load_as_float(dout[(int64_t)place[min(q + k, end - 1)] * ld_dout + c]);
+            for (int w = 0; w < P::W; ++w) to[w] = sum.x[w];
+        }
+    };
+    for (int64_t q = begin; q < end; q += U) {
+        uint2 item[U];
+        P p[U];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (q + k < end) sum += x[k];
+        for (int u = 0; u < U; ++u) item[u] = pair[min(q + u, end - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (item[u].x < (uint32_t)rows) p[u].load(dout + (int64_t)item[u].y * ld_dout + c);
+            else p[u].fill(0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (q + u < end) {
+                if (item[u].x != row) {
+                    leave(true);
+                    row = item[u].x;
+                    whole = true;
+                    sum.fill(0.f);
+                }
+                sum.add(p[u]);
             }
-            dtable[v * ld_dtable + c] = round_to<T>(scale * sum);
         }
     }
+    leave(end == n || pair[end].x != row);
 }
+
+// Rows of several runs.  A workgroup looks at 64 runs and adds up the rows that begin in one of them and go on behind it.
+constexpr int JOIN_RUNS = 64;
+
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(256) void join_runs_kernel(const uint2 *pair, int64_t n, int32_t run, int64_t runs, int64_t rows, int32_t width, float scale, T *dtable,
+                                                        int64_t ld_dtable, const float *part, int32_t part_width, int lanes) {
+    typedef Piece<T, WHOLE> P;
+    __shared__ int32_t head[JOIN_RUNS], last[JOIN_RUNS];
+    __shared__ float shared[256 * P::W];
+    const int64_t first = (int64_t)blockIdx.x * JOIN_RUNS;
+    if (threadIdx.x < JOIN_RUNS) {
+        const int64_t k = first + threadIdx.x;
+        head[threadIdx.x] = -1;
+        if (k + 1 < runs) {
+            const uint32_t row = pair[(k + 1) * run].x;
+            // goes on behind this run, and begins in it
+            if (row < (uint32_t)rows && pair[(k + 1) * run - 1].x == row && (pair[k * run].x != row || k == 0 || pair[k * run - 1].x != row)) {
+                int64_t low = k + 1, high = runs;       // the last run that begins with it
+                while (high - low > 1) {
+                    const int64_t mid = (low + high) / 2;
+                    if (pair[mid * run].x == row) low = mid;
+                    else high = mid;
+                }
+                head[threadIdx.x] = (int32_t)row;
+                last[threadIdx.x] = (int32_t)low;
+            }
+        }
+    }
+    __syncthreads();
+    const int groups = 256 / lanes, group = threadIdx.x / lanes;
+    const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;
+    const bool there = c < width;
+    // short ones: a group of lanes each; long ones: all groups together
+    for (int pass = 0; pass < 2; ++pass)
+        for (int h = pass ? 0 : group; h < JOIN_RUNS; h += pass ? 1 : groups) {
+            if (head[h] < 0) continue;
+            const int64_t k = first + h, count = last[h] - k;      // this run's second sum, and the first sums of `count` runs behind it
+            if ((count > 32) != (pass == 1)) continue;
+            const int64_t each = pass ? (count + groups - 1) / groups : count, begin = pass ? min(count, group * each) : 0, end = min(count, begin + each);
+            P sum;
+            sum.fill(0.f);
+            if (there) {
+                auto add = [&](int64_t at) {
+                    P p;
+#pragma unroll
+                    for (int w = 0; w < P::W; ++w) p.x[w] = part[at * part_width + c + w];
+                    sum.add(p);
+                };
+                if (!pass || group == 0) add(2 * k + 1);
+#pragma unroll 4
+                for (int64_t j = begin; j < end; ++j) add(2 * (k + 1 + j));
+            }
+            if (pass) {
+#pragma unroll
+                for (int w = 0; w < P::W; ++w) shared[w * 256 + threadIdx.x] = sum.x[w];
+                __syncthreads();
+                if (group == 0)
+                    for (int g = 1; g < groups; ++g)
+#pragma unroll
+                        for (int w = 0; w < P::W; ++w) sum.x[w] += shared[w * 256 + g * lanes + threadIdx.x];
+                __syncthreads();
+            }
+            if (there && (!pass || group == 0)) {
+                sum.scale(scale);
+                sum.store(dtable + (int64_t)head[h] * ld_dtable + c);
+            }
+        }
+}
+
+struct Layout {                     // lanes of a row, rows of workgroups for what is wider
+    int lanes;
+    unsigned slices;
+};
+Layout layout(int32_t width, int piece) {
+    const int32_t pieces = (width + piece - 1) / piece;
+    int lanes = 1;
+    while (lanes < WAVE_LANES && lanes < pieces) lanes *= 2;
+    return {lanes, (unsigned)((pieces + lanes - 1) / lanes)};
+}
+
+// Two workgroups for every compute unit, as long as their rows can be told apart in one pass.
+int64_t owned_rows(int64_t rows) { return std::min<int64_t>(std::max<int64_t>((rows + 511) / 512, 1), OWNER_ROWS); }
+// Every owner reads all ids: they come out of the L2s, at some 10 TB/s, so 2^24 of them cost about as much as the launches of the sort.
+bool few_ids(int64_t n, int64_t rows) { return n <= OWNER_MAX_IDS && n * ((rows + OWNER_ROWS - 1) / OWNER_ROWS) <= 1 << 24; }
 
 struct BackwardWork {
-    uint32_t *key[2];
-    int32_t *place[2], *count;
+    uint2 *pair[2];
+    int32_t *count, *totals;
+    float *part;
+    int32_t run, part_width;
+    int64_t runs;
     size_t bytes;
 };
 
-BackwardWork backward_work(void *base, int64_t n) {
-    BackwardWork w;
+// Runs of 8 to 64 pairs: short enough for 2^18 threads of eight elements each, so that loads are in flight on every compute unit.
+BackwardWork backward_work(void *base, int64_t n, int64_t rows, int32_t width) {
+    BackwardWork w{};
+    if (few_ids(n, rows)) return w;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         void *p = reinterpret_cast<char *>(base) + at;
         at += (bytes + 255) / 256 * 256;
         return p;
     };
-    for (int k = 0; k < 2; ++k) {
-        w.key[k] = (uint32_t *)take((size_t)n * 4);
-        w.place[k] = (int32_t *)take((size_t)n * 4);
-    }
+    w.run = 8;
+    while (w.run < 64 && n / w.run * std::min((width + 7) / 8, 64) > 1 << 18) w.run *= 2;
+    w.runs = (n + w.run - 1) / w.run;
+    w.part_width = (width + 7) / 8 * 8;
+    for (uint2 *&p : w.pair) p = (uint2 *)take((size_t)n * sizeof(uint2));
     w.count = (int32_t *)take((size_t)DIGITS * SORT_BLOCKS * 4);
+    w.totals = (int32_t *)take(DIGITS * 4);
+    w.part = (float *)take((size_t)w.runs * 2 * w.part_width * 4);
     w.bytes = at;
     return w;
 }
@@ -179,6 +548,15 @@ int backward_shape(int64_t n, int64_t rows, int32_t width) {
     if (n < 0 || rows < 0 || width < 1) return LIBRA_ERR_SHAPE;
     if (n > INT32_MAX || rows >= INT32_MAX) return LIBRA_ERR_TOO_LARGE;
     return LIBRA_OK;
+}
+
+// f(T, whether every row of the arrays is whole 16-byte pieces)
+template <class F> int for_rows(int dtype, bool whole, F &&f) {
+    return for_dtype(dtype, [&](auto tag) { return whole ? f(tag, std::true_type{}) : f(tag, std::false_type{}); });
+}
+bool whole_rows(const void *p, int64_t ld, int32_t width, int dtype) {
+    const int piece = 16 / (int)dtype_bytes(dtype);
+    return aligned_to(p, 16) && ld % piece == 0 && width % piece == 0;
 }
 
 }  // namespace
@@ -191,11 +569,13 @@ extern "C" int libra_embedding(const void *table, int64_t rows, int32_t width, i
     if (n == 0) return LIBRA_OK;
     if (!index || !out || (!table && rows > 0)) return LIBRA_ERR_NULL;
     if (!aligned_to(table, dtype_bytes(dtype)) || !aligned_to(out, dtype_bytes(dtype)) || !aligned_to(index, index_bytes(index_type))) return LIBRA_ERR_BUFFER;
-    const unsigned blocks = (unsigned)std::min<int64_t>((n + 3) / 4, 1 << 16);
-    return for_dtype(dtype, [&](auto tag) {
+    return for_rows(dtype, whole_rows(table, ld_table, width, dtype) && whole_rows(out, ld_out, width, dtype), [&](auto tag, auto whole) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((embedding_kernel<T>), dim3(blocks), dim3(256), 0, (hipStream_t)stream, (const T *)table, rows, width, ld_table, index, index_type, n, scale,
-                           (T *)out, ld_out);
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int lanes = layout(width, Piece<T, WHOLE>::W).lanes;
+        const int64_t each = 256 / lanes * LOOKUP_ROWS;
+        hipLaunchKernelGGL((embedding_kernel<T, WHOLE>), dim3((unsigned)std::min<int64_t>((n + each - 1) / each, 1 << 20)), dim3(256), 0, (hipStream_t)stream,
+                           (const T *)table, rows, width, ld_table, index, index_type, n, scale, (T *)out, ld_out, lanes);
         return last_launch();
     });
 }
@@ -203,7 +583,7 @@ extern "C" int libra_embedding(const void *table, int64_t rows, int32_t width, i
 extern "C" int libra_embedding_backward_workspace(int64_t n, int64_t rows, int32_t width, size_t *bytes) {
     if (!bytes) return LIBRA_ERR_NULL;
     if (int rc = backward_shape(n, rows, width)) return rc;
-    *bytes = backward_work(nullptr, n).bytes;
+    *bytes = backward_work(nullptr, n, rows, width).bytes;
     return LIBRA_OK;
 }
 
@@ -214,29 +594,52 @@ extern "C" int libra_embedding_backward(const void *dout, int64_t ld_dout, int d
     if (!known_dtype(dtype)) return LIBRA_ERR_DTYPE;
     if (!known_index(index_type)) return LIBRA_ERR_OPTION;
     if (rows == 0) return LIBRA_OK;
-    if (!dtable || ((!dout || !index || !workspace) && n > 0)) return LIBRA_ERR_NULL;
+    const BackwardWork w = backward_work(workspace, n, rows, width);
+    if (!dtable || ((!dout || !index) && n > 0) || (!workspace && w.bytes > 0)) return LIBRA_ERR_NULL;
     if (!aligned_to(dout, dtype_bytes(dtype)) || !aligned_to(dtable, dtype_bytes(dtype)) || !aligned_to(index, index_bytes(index_type))) return LIBRA_ERR_BUFFER;
-    const BackwardWork w = backward_work(workspace, n);
-    if (n > 0 && (workspace_bytes < w.bytes || !aligned_to(workspace, 256))) return LIBRA_ERR_BUFFER;
+    if (w.bytes > 0 && (workspace_bytes < w.bytes || !aligned_to(workspace, 256))) return LIBRA_ERR_BUFFER;
     hipStream_t s = (hipStream_t)stream;
-    int at = 0;
-    if (n > 0) {
-        const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE, blocks = std::min<int64_t>(tiles, SORT_BLOCKS), each = (tiles + blocks - 1) / blocks * SORT_TILE;
-        Keys in{index, index_type, rows, nullptr, nullptr};
-        for (int shift = 0; shift == 0 || rows >> shift; shift += 8, at ^= 1) {
-            hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, w.count);
-            hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, w.count, DIGITS * (int)blocks);
-            hipLaunchKernelGGL(sort_place_kernel, dim3((unsigned)blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, w.count, w.key[at], w.place[at]);
-            in.key = w.key[at];
-            in.place = w.place[at];
-        }
-        at ^= 1;
-    }
-    const unsigned blocks = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16);
-    return for_dtype(dtype, [&](auto tag) {
+    const bool pieces = whole_rows(dout, ld_dout, width, dtype) && whole_rows(dtable, ld_dtable, width, dtype);
+    if (few_ids(n, rows)) return for_rows(dtype, pieces, [&](auto tag, auto whole) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((embedding_sum_kernel<T>), dim3(blocks), dim3(256), 0, s, (const T *)dout, ld_dout, w.key[at], w.place[at], n, rows, width, scale, (T *)dtable,
-                           ld_dtable);
+        constexpr bool WHOLE = decltype(whole)::value;
+        const Layout l = layout(width, Piece<T, WHOLE>::W);
+        const int64_t owned = owned_rows(rows);
+        const dim3 grid((unsigned)((rows + owned - 1) / owned), l.slices);
+        auto launch = [&](auto most) {
+            hipLaunchKernelGGL((owner_kernel<T, WHOLE, decltype(most)::value>), grid, dim3(OWNER_THREADS), 0, s, (const T *)dout, ld_dout, index, index_type, (int32_t)n, rows, width,
+                               (int32_t)owned, scale, (T *)dtable, ld_dtable, l.lanes);
+        };
+        // two workgroups on a compute unit with half a list, one with a whole one
+        if (n <= OWNER_MAX_IDS / 2) launch(std::integral_constant<int, OWNER_MAX_IDS / 2>{});
+        else launch(std::integral_constant<int, OWNER_MAX_IDS>{});
+        return last_launch();
+    });
+    int bits = 1;
+    while (rows >> bits) ++bits;
+    const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
+    const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE, per = (tiles + SORT_BLOCKS - 1) / SORT_BLOCKS, each = per * SORT_TILE;
+    const unsigned blocks = (unsigned)((tiles + per - 1) / per);
+    Keys in{index, index_type, rows, nullptr};
+    const size_t size = dtype_bytes(dtype);
+    for (int p = 0, shift = 0; p < passes; ++p) {
+        const int digit = (bits - shift + passes - p - 1) / (passes - p);
+        const Zeros zeros{(char *)dtable, rows, (int64_t)width * (int64_t)size, ld_dtable * (int64_t)size, p == 0 ? 2048u : 0u};
+        hipLaunchKernelGGL(sort_count_kernel, dim3(blocks + zeros.blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, digit, blocks, w.count, zeros);
+        hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((1 << digit) + SCAN_DIGITS - 1) / SCAN_DIGITS), dim3(1024), 0, s, w.count, (int)blocks, w.totals);
+        hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, digit, w.count, w.totals, w.pair[p & 1]);
+        in.pair = w.pair[p & 1];
+        shift += digit;
+    }
+    return for_rows(dtype, pieces, [&](auto tag, auto whole) {
+        typedef decltype(tag) T;
+        constexpr bool WHOLE = decltype(whole)::value;
+        const Layout l = layout(width, Piece<T, WHOLE>::W);
+        const int groups = 256 / l.lanes;
+        hipLaunchKernelGGL((run_sums_kernel<T, WHOLE>), dim3((unsigned)((w.runs + groups - 1) / groups), l.slices), dim3(256), 0, s, (const T *)dout, ld_dout, in.pair, n, w.run, rows,
+                           width, scale, (T *)dtable, ld_dtable, w.part, w.part_width, l.lanes);
+        hipLaunchKernelGGL((join_runs_kernel<T, WHOLE>), dim3((unsigned)((w.runs + JOIN_RUNS - 1) / JOIN_RUNS), l.slices), dim3(256), 0, s, in.pair, n, w.run, w.runs, rows, width,
+                           scale, (T *)dtable, ld_dtable, w.part, w.part_width, l.lanes);
         return last_launch();
     });
 }
