@@ -46,16 +46,17 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T *table, int64_t 
     const int32_t pieces = width / P::W;
     for (int64_t first = (int64_t)blockIdx.x * (groups * LOOKUP_ROWS); first < n; first += (int64_t)gridDim.x * (groups * LOOKUP_ROWS)) {
         int64_t v[LOOKUP_ROWS];
-#pragma unroll
-        for (int u = 0; u < LOOKUP_ROWS; ++u) v[u] = index_at(index, index_type, min(first + u * groups + group, n - 1));
+        indices_at<LOOKUP_ROWS>(index, index_type, [&](int u) { return min(first + u * groups + group, n - 1); }, v);
         for (int32_t c = lane; c < pieces; c += lanes) {
             P p[LOOKUP_ROWS];
+            if (rows > 0) {                 // (loads from some row even where there is none to load: a load in a branch would wait for those before it)
+#pragma unroll
+                for (int u = 0; u < LOOKUP_ROWS; ++u) p[u].load(table + (v[u] >= 0 && v[u] < rows ? v[u] : 0) * ld_table + c * P::W);
+            }
 #pragma unroll
             for (int u = 0; u < LOOKUP_ROWS; ++u) {
-                if (v[u] >= 0 && v[u] < rows) {
-                    p[u].load(table + v[u] * ld_table + c * P::W);
-                    p[u].scale(scale);
-                } else p[u].fill(v[u] == -1 ? 0.f : __builtin_nanf(""));
+                p[u].scale(scale);
+                if (v[u] < 0 || v[u] >= rows) p[u].fill(v[u] == -1 ? 0.f : __builtin_nanf(""));
             }
 #pragma unroll
             for (int u = 0; u < LOOKUP_ROWS; ++u)
@@ -86,26 +87,30 @@ __device__ inline uint64_t same_digit(uint32_t digit, int bits, bool real) {
     return real ? same : 0;
 }
 // Number of this digit in the wave so far (counted in LDS, where only this wave counts), among earlier batches and lower lanes
-__device__ inline int32_t rank_in_wave(uint32_t digit, int bits, bool real, int32_t *count) {
+template <class C> __device__ inline int32_t rank_in_wave(uint32_t digit, int bits, bool real, C *count) {
     const int lane = threadIdx.x % WAVE_LANES;
     const uint64_t same = same_digit(digit, bits, real);
     const int before = __popcll(same & ((1ull << lane) - 1));
-    int32_t base = 0;
-    if (real && before == 0) base = atomicAdd(&count[digit], (int32_t)__popcll(same));
-    return __shfl(base, real ? __ffsll((unsigned long long)same) - 1 : 0) + before;
+    volatile C *c = count + digit;
+    const int32_t base = real ? *c : 0;
+    __builtin_amdgcn_wave_barrier();                // all lanes have read before one writes: a wave's LDS accesses keep their order
+    if (real && before == 0) *c = (C)(base + __popcll(same));
+    __builtin_amdgcn_wave_barrier();
+    return base + before;
 }
 
 // -- few ids --
-constexpr int OWNER_THREADS = 1024, OWNER_WAVES = OWNER_THREADS / WAVE_LANES, OWNER_IDS = 16, OWNER_PLACE_BITS = 14, OWNER_MAX_IDS = 1 << OWNER_PLACE_BITS;
+constexpr int OWNER_THREADS = 1024, OWNER_WAVES = OWNER_THREADS / WAVE_LANES, OWNER_PLACE_BITS = 14, OWNER_MAX_IDS = 1 << OWNER_PLACE_BITS;
 constexpr int OWNER_ROW_BITS = 9, OWNER_ROWS = 1 << OWNER_ROW_BITS, OWNER_LONG = 32;    // rows with more ids than that are added up by the whole workgroup
-static_assert(OWNER_THREADS * OWNER_IDS == OWNER_MAX_IDS, "a thread holds its share of a full list");
 
 template <class T, bool WHOLE, int MOST>
 __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int64_t ld_dout, const void *index, int index_type, int32_t n, int64_t rows, int32_t width,
                                                               int32_t owned, float scale, T *dtable, int64_t ld_dtable, int lanes) {
     typedef Piece<T, WHOLE> P;
+    constexpr int IDS = MOST / OWNER_THREADS;
     __shared__ uint32_t list[MOST];                             // row in this run << OWNER_PLACE_BITS | place, n at most
     __shared__ int32_t start[OWNER_ROWS], total[OWNER_WAVES], long_rows[OWNER_MAX_IDS / OWNER_LONG], longs;
+    __shared__ uint8_t named[OWNER_ROWS];                       // the row has ids
     __shared__ union {                                          // first the one, then the other
         int32_t count[OWNER_WAVES][OWNER_ROWS];
         float part[OWNER_THREADS * 8];
@@ -116,20 +121,24 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
     const int64_t low = (int64_t)blockIdx.x * owned;
     const int32_t mine = (int32_t)min((int64_t)owned, rows - low);
 
+    const int groups = OWNER_THREADS / lanes, group = threadIdx.x / lanes;
+    const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;        // this lane's columns
+    const bool there = c < width;
+    for (int r = threadIdx.x; r < OWNER_ROWS; r += OWNER_THREADS) named[r] = 0;
+
     // the ids of these rows, in the order of their places
     int32_t m = 0;
     {
-        const int32_t each = (n + OWNER_THREADS - 1) / OWNER_THREADS;
-        uint32_t row[OWNER_IDS];
+        uint32_t row[IDS];
+        int64_t v[IDS];
         int32_t found = 0;
+        const int32_t each = (n + OWNER_THREADS - 1) / OWNER_THREADS, at = wave * each * WAVE_LANES + lane;
+        if (n > 0) indices_at<IDS>(index, index_type, [&](int b) { return min(at + min(b, each - 1) * WAVE_LANES, n - 1); }, v);
 #pragma unroll
-        for (int b = 0; b < OWNER_IDS; ++b) {
-            const int32_t i = (wave * each + b) * WAVE_LANES + lane;
-            const int64_t v = b < each && i < n ? index_at(index, index_type, i) - low : -1;
-            row[b] = v >= 0 && v < mine ? (uint32_t)v : ~0u;
+        for (int b = 0; b < IDS; ++b) {
+            row[b] = b < each && at + b * WAVE_LANES < n && v[b] >= low && v[b] < low + mine ? (uint32_t)(v[b] - low) : ~0u;
+            found += __popcll(__ballot(row[b] != ~0u));
         }
-#pragma unroll
-        for (int b = 0; b < OWNER_IDS; ++b) found += __popcll(__ballot(row[b] != ~0u));
         if (lane == 0) total[wave] = found;
         __syncthreads();
         int32_t to = 0;
@@ -139,23 +148,32 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
             m += t;
         }
 #pragma unroll
-        for (int b = 0; b < OWNER_IDS; ++b) {
+        for (int b = 0; b < IDS; ++b) {
             const uint64_t those = __ballot(row[b] != ~0u);
-            if (row[b] != ~0u) list[to + __popcll(those & ((1ull << lane) - 1))] = row[b] << OWNER_PLACE_BITS | (uint32_t)((wave * each + b) * WAVE_LANES + lane);
+            if (row[b] != ~0u) {
+                list[to + __popcll(those & ((1ull << lane) - 1))] = row[b] << OWNER_PLACE_BITS | (uint32_t)(at + b * WAVE_LANES);
+                named[row[b]] = 1;
+            }
             to += __popcll(those);
         }
     }
     for (int r = threadIdx.x; r < OWNER_WAVES * OWNER_ROWS; r += OWNER_THREADS) (&count[0][0])[r] = 0;
     if (threadIdx.x == 0) longs = 0;
     __syncthreads();
+    if (there) {                                                // the zeros, on their way while the list is sorted
+        P zero;
+        zero.fill(0.f);
+        for (int32_t r = group; r < mine; r += groups)
+            if (!named[r]) zero.store(dtable + (low + r) * ld_dtable + c);
+    }
 
     // into the order of their rows (`start`: where a row's ids begin)
     {
         const int32_t each = (m + OWNER_THREADS - 1) / OWNER_THREADS;
-        uint32_t item[OWNER_IDS];
-        int32_t rank[OWNER_IDS];
+        uint32_t item[IDS];
+        int32_t rank[IDS];
 #pragma unroll
-        for (int b = 0; b < OWNER_IDS; ++b) {
+        for (int b = 0; b < IDS; ++b) {
             if (b < each) {
                 const int32_t q = (wave * each + b) * WAVE_LANES + lane;
                 item[b] = q < m ? list[q] : 0;
@@ -182,7 +200,7 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
         if (threadIdx.x < OWNER_ROWS) start[threadIdx.x] = up_to - sum;
         __syncthreads();
 #pragma unroll
-        for (int b = 0; b < OWNER_IDS; ++b) {
+        for (int b = 0; b < IDS; ++b) {
             const int32_t q = (wave * each + b) * WAVE_LANES + lane;
             if (b < each && q < m) {
                 const int32_t r = item[b] >> OWNER_PLACE_BITS;
@@ -192,16 +210,12 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
         __syncthreads();
     }
 
-    const int groups = OWNER_THREADS / lanes, group = threadIdx.x / lanes;
-    const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;        // this lane's columns
-    const bool there = c < width;
     auto end_of = [&](int32_t r) { return r + 1 < OWNER_ROWS ? start[r + 1] : m; };
     auto sum_of = [&](int32_t q, int32_t end, P &sum) {                          // four rows in flight
         for (; q < end; q += 4) {
             P p[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (q + u < end) p[u].load(dout + (int64_t)(list[q + u] & (OWNER_MAX_IDS - 1)) * ld_dout + c);
+            for (int u = 0; u < 4; ++u) p[u].load(dout + (int64_t)(list[min(q + u, end - 1)] & (OWNER_MAX_IDS - 1)) * ld_dout + c);
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (q + u < end) sum.add(p[u]);
@@ -213,7 +227,7 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
             if (threadIdx.x % lanes == 0) long_rows[atomicAdd(&longs, 1)] = r;
             continue;
         }
-        if (!there) continue;
+        if (!there || begin == end) continue;
         P sum;
         sum.fill(0.f);
         sum_of(begin, end, sum);
@@ -242,8 +256,8 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
 }
 
 // -- many ids: pairs sorted by row, up to 11 bits at a time; equal rows keep the order of their places --
-constexpr int DIGIT_BITS = 11, DIGITS = 1 << DIGIT_BITS, SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / WAVE_LANES, SORT_BATCHES = 16;
-constexpr int SORT_TILE = SORT_THREADS * SORT_BATCHES, SORT_BLOCKS = 512, SCAN_DIGITS = WAVE_LANES;
+constexpr int DIGIT_BITS = 11, DIGITS = 1 << DIGIT_BITS, SORT_THREADS = 256, PLACE_THREADS = 1024, PLACE_WAVES = PLACE_THREADS / WAVE_LANES, PLACE_BATCHES = 4;
+constexpr int SORT_TILE = PLACE_THREADS * PLACE_BATCHES, SORT_BLOCKS = 512, SCAN_DIGITS = WAVE_LANES;
 
 struct Keys {                       // of one pass: the ids themselves in the first one, pairs afterwards
     const void *index;
@@ -321,16 +335,30 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(int32_t *count, int blo
     }
 }
 
-__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, const int32_t *count, const int32_t *totals, uint2 *out) {
-    __shared__ int32_t next[DIGITS], mine[SORT_WAVES][DIGITS], part[SORT_WAVES];
+// A tile of 4,096 pairs at a time: their numbers among the tile's pairs of the same digit, wave by wave, and from there their places.
+// Many waves of few pairs: ranking is a chain of ballots and LDS accesses (four waves of 16 pairs a lane took 15 us for a tile, not 7).
+__global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, const int32_t *count, const int32_t *totals, uint2 *out) {
+    __shared__ int32_t next[DIGITS], part[PLACE_WAVES];
+    __shared__ uint16_t mine[PLACE_WAVES][DIGITS];               // pairs of each wave, then of the waves before it: below 4,096
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES, digits = 1 << bits;
+    constexpr int EACH = DIGITS / PLACE_THREADS;
     {   // where this block's first pair of each digit goes: totals of the digits before, and what earlier blocks have
-        constexpr int EACH = DIGITS / SORT_THREADS;
-        int32_t t[EACH], sum = 0;
+        int32_t t[EACH], earlier[EACH], sum = 0;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
             const int d = threadIdx.x * EACH + k;
-            t[k] = d < digits ? totals[d] : 0;
+            t[k] = earlier[k] = 0;
+            if (d < digits && totals) {
+                t[k] = totals[d];
+                earlier[k] = count[(int64_t)blockIdx.x * DIGITS + d];
+            } else if (d < digits) {
+#pragma unroll 8
+                for (int b = 0; b < (int)gridDim.x; ++b) {
+                    const int32_t x = count[(int64_t)b * DIGITS + d];
+                    t[k] += x;
+                    earlier[k] += b < (int)blockIdx.x ? x : 0;
+                }
+            }
             sum += t[k];
         }
         int32_t up_to = sum;
@@ -345,36 +373,46 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(Keys in, int64
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
             const int d = threadIdx.x * EACH + k;
-            next[d] = d < digits ? up_to + count[(int64_t)blockIdx.x * DIGITS + d] : 0;
+            next[d] = up_to + earlier[k];
             up_to += t[k];
         }
     }
     const int64_t begin = (int64_t)blockIdx.x * each, end = min(n, begin + each);
     for (int64_t tile = begin; tile < end; tile += SORT_TILE) {
-        for (int d = threadIdx.x; d < SORT_WAVES * DIGITS; d += SORT_THREADS) (&mine[0][0])[d] = 0;
-        __syncthreads();
-        uint2 pair[SORT_BATCHES];
-        int32_t rank[SORT_BATCHES];
-        const int64_t at = tile + (int64_t)wave * (SORT_BATCHES * WAVE_LANES) + lane;
+        uint2 pair[PLACE_BATCHES];
+        int32_t rank[PLACE_BATCHES], all[EACH];
+        const int64_t at = tile + (int64_t)wave * (PLACE_BATCHES * WAVE_LANES) + lane;
 #pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b) pair[b] = in.at(min(at + b * WAVE_LANES, end - 1));
-#pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b) rank[b] = rank_in_wave((pair[b].x >> shift) & (digits - 1), bits, at + b * WAVE_LANES < end, mine[wave]);
+        for (int b = 0; b < PLACE_BATCHES; ++b) pair[b] = in.at(min(at + b * WAVE_LANES, end - 1));
+        for (int w = 0; w < PLACE_WAVES; ++w)
+            for (int d = threadIdx.x; d < (digits + 1) / 2; d += PLACE_THREADS) reinterpret_cast<uint32_t *>(mine[w])[d] = 0;
         __syncthreads();
-        for (int d = threadIdx.x; d < digits; d += SORT_THREADS) {
-            int32_t place = next[d];
-            for (int w = 0; w < SORT_WAVES; ++w) {
-                const int32_t c = mine[w][d];
-                mine[w][d] = place;
-                place += c;
+#pragma unroll
+        for (int b = 0; b < PLACE_BATCHES; ++b) rank[b] = rank_in_wave((pair[b].x >> shift) & (digits - 1), bits, at + b * WAVE_LANES < end, mine[wave]);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int d = k * PLACE_THREADS + threadIdx.x;
+            uint16_t c[PLACE_WAVES];
+            all[k] = 0;
+            if (d >= digits) continue;
+#pragma unroll
+            for (int w = 0; w < PLACE_WAVES; ++w) c[w] = mine[w][d];
+#pragma unroll
+            for (int w = 0; w < PLACE_WAVES; ++w) {
+                mine[w][d] = (uint16_t)all[k];
+                all[k] += c[w];
             }
-            next[d] = place;
         }
         __syncthreads();
 #pragma unroll
-        for (int b = 0; b < SORT_BATCHES; ++b)
-            if (at + b * WAVE_LANES < end) out[mine[wave][(pair[b].x >> shift) & (digits - 1)] + rank[b]] = pair[b];
+        for (int b = 0; b < PLACE_BATCHES; ++b) {
+            const int d = (pair[b].x >> shift) & (digits - 1);
+            if (at + b * WAVE_LANES < end) out[next[d] + mine[wave][d] + rank[b]] = pair[b];
+        }
         __syncthreads();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) next[k * PLACE_THREADS + threadIdx.x] += all[k];
     }
 }
 
@@ -409,9 +447,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld
 #pragma unroll
         for (int u = 0; u < U; ++u) item[u] = pair[min(q + u, end - 1)];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (item[u].x < (uint32_t)rows) p[u].load(dout + (int64_t)item[u].y * ld_dout + c);
-            else p[u].fill(0.f);
+        for (int u = 0; u < U; ++u) p[u].load(dout + (int64_t)item[u].y * ld_dout + c);       // (also of padding: its sum goes nowhere)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (q + u < end) {
@@ -428,73 +464,109 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld
     leave(end == n || pair[end].x != row);
 }
 
-// Rows of several runs.  A workgroup looks at 64 runs and adds up the rows that begin in one of them and go on behind it.
-constexpr int JOIN_RUNS = 64;
+// Rows of several runs.  A workgroup looks at 64 runs and adds up the rows that begin in one of them and go on behind it: a group of lanes
+// each, which walks on while runs begin with the row; all groups together those that reach over more than 32 runs.
+constexpr int JOIN_RUNS = 64, LONG_JOIN = 32;
 
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(256) void join_runs_kernel(const uint2 *pair, int64_t n, int32_t run, int64_t runs, int64_t rows, int32_t width, float scale, T *dtable,
                                                         int64_t ld_dtable, const float *part, int32_t part_width, int lanes) {
     typedef Piece<T, WHOLE> P;
-    __shared__ int32_t head[JOIN_RUNS], last[JOIN_RUNS];
+    constexpr int U = 4;
+    __shared__ int64_t head[JOIN_RUNS];                         // row; as ~row if it is a long one; 2^40 for none
     __shared__ float shared[256 * P::W];
+    __shared__ uint64_t shorts, longs;                          // which of the runs
+    __shared__ unsigned equal;
+    static_assert(JOIN_RUNS == WAVE_LANES, "a wave looks at them");
+    constexpr int64_t NONE = 1ll << 40;
     const int64_t first = (int64_t)blockIdx.x * JOIN_RUNS;
     if (threadIdx.x < JOIN_RUNS) {
         const int64_t k = first + threadIdx.x;
-        head[threadIdx.x] = -1;
+        int64_t h = NONE;
         if (k + 1 < runs) {
-            const uint32_t row = pair[(k + 1) * run].x;
-            // goes on behind this run, and begins in it
-            if (row < (uint32_t)rows && pair[(k + 1) * run - 1].x == row && (pair[k * run].x != row || k == 0 || pair[k * run - 1].x != row)) {
-                int64_t low = k + 1, high = runs;       // the last run that begins with it
-                while (high - low > 1) {
-                    const int64_t mid = (low + high) / 2;
-                    if (pair[mid * run].x == row) low = mid;
-                    else high = mid;
-                }
-                head[threadIdx.x] = (int32_t)row;
-                last[threadIdx.x] = (int32_t)low;
-            }
+            const int64_t beyond = min(k + 1 + LONG_JOIN, runs - 1);
+            const uint32_t row = pair[(k + 1) * run].x, end = pair[(k + 1) * run - 1].x, begin = pair[k * run].x, before = pair[max(k * run - 1, (int64_t)0)].x, far = pair[beyond * run].x;
+            if (row < (uint32_t)rows && end == row && (begin != row || before != row || k == 0)) h = far == row && beyond == k + 1 + LONG_JOIN ? ~(int64_t)row : (int64_t)row;
         }
+        head[threadIdx.x] = h;
+        const uint64_t here = __ballot(h >= 0 && h != NONE), reaching = __ballot(h < 0);
+        if (threadIdx.x == 0) shorts = here, longs = reaching;
     }
     __syncthreads();
     const int groups = 256 / lanes, group = threadIdx.x / lanes;
     const int32_t c = (blockIdx.y * lanes + threadIdx.x % lanes) * P::W;
     const bool there = c < width;
-    // short ones: a group of lanes each; long ones: all groups together
-    for (int pass = 0; pass < 2; ++pass)
-        for (int h = pass ? 0 : group; h < JOIN_RUNS; h += pass ? 1 : groups) {
-            if (head[h] < 0) continue;
-            const int64_t k = first + h, count = last[h] - k;      // this run's second sum, and the first sums of `count` runs behind it
-            if ((count > 32) != (pass == 1)) continue;
-            const int64_t each = pass ? (count + groups - 1) / groups : count, begin = pass ? min(count, group * each) : 0, end = min(count, begin + each);
-            P sum;
-            sum.fill(0.f);
-            if (there) {
-                auto add = [&](int64_t at) {
-                    P p;
+    auto load = [&](int64_t at) {
+        P p;
 #pragma unroll
-                    for (int w = 0; w < P::W; ++w) p.x[w] = part[at * part_width + c + w];
-                    sum.add(p);
-                };
-                if (!pass || group == 0) add(2 * k + 1);
-#pragma unroll 4
-                for (int64_t j = begin; j < end; ++j) add(2 * (k + 1 + j));
+        for (int w = 0; w < P::W; ++w) p.x[w] = part[at * part_width + c + w];
+        return p;
+    };
+    if (there)
+        for (int h = group; h < JOIN_RUNS; h += groups) {
+            if (!(shorts >> h & 1)) continue;
+            const int64_t row = head[h];
+            P sum = load(2 * (first + h) + 1);                  // what this run left for the row behind its end, and the first sums of those behind
+            for (int64_t j = first + h + 1, more = 1; more; j += U) {
+                uint32_t key[U];
+                P p[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t at = min(j + u, runs - 1);
+                    key[u] = pair[at * run].x;
+                    p[u] = load(2 * at);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    more = more && j + u < runs && key[u] == (uint32_t)row;
+                    if (more) sum.add(p[u]);
+                }
             }
-            if (pass) {
+            sum.scale(scale);
+            sum.store(dtable + row * ld_dtable + c);
+        }
+    for (uint64_t those = longs; those; those &= those - 1) {   // the same for the whole workgroup
+        const int h = __ffsll((unsigned long long)those) - 1;
+        const int64_t row = ~head[h], k = first + h;
+        int64_t low = k + 1, high = runs;                       // the last run that begins with the row: 256 places at a time
+        while (high - low > 1) {
+            const int64_t step = (high - low + 255) / 256, at = low + threadIdx.x * step;
+            if (threadIdx.x == 0) equal = 0;
+            __syncthreads();
+            const uint64_t with = __ballot(at < high && pair[min(at, runs - 1) * run].x == (uint32_t)row);
+            if (threadIdx.x % WAVE_LANES == 0) atomicAdd(&equal, (unsigned)__popcll(with));
+            __syncthreads();
+            const int64_t found = equal;                        // at least one: low itself
+            high = min(high, low + found * step);
+            low += (found - 1) * step;
+            __syncthreads();
+        }
+        const int64_t count = low - k, each = (count + groups - 1) / groups, begin = min(count, group * each), end = min(count, begin + each);
+        P sum;
+        sum.fill(0.f);
+        if (there) {
+            if (group == 0) sum = load(2 * k + 1);
+            for (int64_t j = begin; j < end; j += U) {
+                P p[U];
 #pragma unroll
-                for (int w = 0; w < P::W; ++w) shared[w * 256 + threadIdx.x] = sum.x[w];
-                __syncthreads();
-                if (group == 0)
-                    for (int g = 1; g < groups; ++g)
+                for (int u = 0; u < U; ++u) p[u] = load(2 * (k + 1 + min(j + u, end - 1)));
 #pragma unroll
-                        for (int w = 0; w < P::W; ++w) sum.x[w] += shared[w * 256 + g * lanes + threadIdx.x];
-                __syncthreads();
-            }
-            if (there && (!pass || group == 0)) {
-                sum.scale(scale);
-                sum.store(dtable + (int64_t)head[h] * ld_dtable + c);
+                for (int u = 0; u < U; ++u)
+                    if (j + u < end) sum.add(p[u]);
             }
         }
+#pragma unroll
+        for (int w = 0; w < P::W; ++w) shared[w * 256 + threadIdx.x] = sum.x[w];
+        __syncthreads();
+        if (group == 0 && there) {
+            for (int g = 1; g < groups; ++g)
+#pragma unroll
+                for (int w = 0; w < P::W; ++w) sum.x[w] += shared[w * 256 + g * lanes + threadIdx.x];
+            sum.scale(scale);
+            sum.store(dtable + row * ld_dtable + c);
+        }
+        __syncthreads();
+    }
 }
 
 struct Layout {                     // lanes of a row, rows of workgroups for what is wider
@@ -620,14 +692,15 @@ extern "C" int libra_embedding_backward(const void *dout, int64_t ld_dout, int d
     const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
     const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE, per = (tiles + SORT_BLOCKS - 1) / SORT_BLOCKS, each = per * SORT_TILE;
     const unsigned blocks = (unsigned)((tiles + per - 1) / per);
+    const bool scan = blocks > 32;              // every block of the next launch can add the counts of so few up by itself: 3 us less
     Keys in{index, index_type, rows, nullptr};
     const size_t size = dtype_bytes(dtype);
     for (int p = 0, shift = 0; p < passes; ++p) {
         const int digit = (bits - shift + passes - p - 1) / (passes - p);
         const Zeros zeros{(char *)dtable, rows, (int64_t)width * (int64_t)size, ld_dtable * (int64_t)size, p == 0 ? 2048u : 0u};
         hipLaunchKernelGGL(sort_count_kernel, dim3(blocks + zeros.blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, digit, blocks, w.count, zeros);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((1 << digit) + SCAN_DIGITS - 1) / SCAN_DIGITS), dim3(1024), 0, s, w.count, (int)blocks, w.totals);
-        hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, digit, w.count, w.totals, w.pair[p & 1]);
+        if (scan) hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((1 << digit) + SCAN_DIGITS - 1) / SCAN_DIGITS), dim3(1024), 0, s, w.count, (int)blocks, w.totals);
+        hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(PLACE_THREADS), 0, s, in, n, each, shift, digit, w.count, scan ? w.totals : nullptr, w.pair[p & 1]);
         in.pair = w.pair[p & 1];
         shift += digit;
     }

@@ -69,6 +69,20 @@ __device__ inline int64_t index_at(const void *index, int index_type, int64_t i)
     return index_type == LIBRA_INDEX_I64 ? reinterpret_cast<const int64_t *>(index)[i] : (int64_t)reinterpret_cast<const int32_t *>(index)[i];
 }
 
+// N of them, index_of(k) for each: the loads are issued together
+template <int N, class F> __device__ inline void indices_at(const void *index, int index_type, F &&index_of, int64_t *out) {
+    if (index_type == LIBRA_INDEX_I64) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) out[k] = reinterpret_cast<const int64_t *>(index)[index_of(k)];
+    } else {
+        int32_t x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = reinterpret_cast<const int32_t *>(index)[index_of(k)];
+#pragma unroll
+        for (int k = 0; k < N; ++k) out[k] = x[k];
+    }
+}
+
 inline bool known_index(int index_type) { return index_type == LIBRA_INDEX_I32 || index_type == LIBRA_INDEX_I64; }
 inline size_t index_bytes(int index_type) { return index_type == LIBRA_INDEX_I64 ? 8 : 4; }
 

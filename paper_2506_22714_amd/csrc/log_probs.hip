@@ -235,10 +235,16 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
         // 16-byte pieces of memory: the first and the last may hold other things beside the row
         const int before = (int)((uintptr_t)x % 16 / sizeof(T));
         const int64_t pieces = (before + f.classes + W - 1) / W, each = (pieces + parts.count - 1) / parts.count, begin = part * each, end = min(pieces, begin + each);
-        auto fetch = [&](int64_t v, uint4 *raw) {
+        auto fetch = [&](int64_t v0, uint4 *raw) {
+            if (v0 >= end) return;
+            if ((before == 0 || v0 > begin || part > 0) && v0 + U * LONG_THREADS <= end && (v0 + U * LONG_THREADS) * W <= before + f.classes) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + (v0 + u * LONG_THREADS + threadIdx.x) * W - before);
+                return;
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t p = v + u * LONG_THREADS, j = p * W - before;
+                const int64_t p = v0 + threadIdx.x + u * LONG_THREADS, j = p * W - before;
                 if (p < end && j >= 0 && j + W <= f.classes) raw[u] = *reinterpret_cast<const uint4 *>(x + j);
                 else {
                     float y[W];
@@ -251,10 +257,10 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
         Sums a;
         Best best;
         uint4 raw[U], next[U];
-        fetch(begin + threadIdx.x, raw);
+        fetch(begin, raw);
         for (int64_t v0 = begin; v0 < end; v0 += U * LONG_THREADS) {
             const int64_t v = v0 + threadIdx.x;
-            fetch(v + U * LONG_THREADS, next);          // on its way while this one is worked on
+            fetch(v0 + U * LONG_THREADS, next);         // on its way while this one is worked on
             float y[N];
 #pragma unroll
             for (int u = 0; u < U; ++u) unpack<T>(raw[u], y + u * W);
