@@ -196,8 +196,26 @@ struct Best {
             limit = read_lane(key, top - 1);
         }
     }
-    __device__ float threshold() const { return limit ? logit_of((uint32_t)(limit >> 32)) : -INF; }
 };
+
+// The largest rank of the wave, in a scalar register
+__device__ inline uint32_t wave_most(uint32_t x) {
+    x = over_group<16>(x, [](uint32_t p, uint32_t q) { return max(p, q); });
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, true));     // row_bcast:15
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, true));     // row_bcast:31
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, WAVE_LANES - 1);
+}
+// The k-th largest of the lanes' ranks
+__device__ inline uint32_t wave_kth(uint32_t x, int k) {
+    for (;;) {
+        const uint32_t most = wave_most(x);
+        const uint64_t those = __ballot(x == most);
+        k -= (int)__popcll(those);
+        if (k <= 0 || most == 0) return most;
+        if (x == most) x = 0;
+    }
+}
+__device__ inline float threshold(uint32_t rank) { return rank ? logit_of(rank) : -INF; }
 
 // The `top` best of `lists` descending lists of `top` keys in LDS, by one wave: f(a, key), the same key in every lane.
 template <class F> __device__ inline void merge_lists(const uint64_t *keys, int lists, int top, F &&f) {
@@ -226,6 +244,8 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
     constexpr int W = VECTOR<T>, U = 16 / W, N = U * W;
     __shared__ float shared_sums[LONG_WAVES][3];
     __shared__ uint64_t shared_keys[LONG_WAVES * MAX_TOP];
+    __shared__ uint32_t shared_floor[LONG_WAVES];
+    const int share = (f.top + LONG_WAVES - 1) / LONG_WAVES;
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
     const float c = f.scale * LOG2E;
     for (int64_t unit = blockIdx.x; unit < f.n * parts.count; unit += gridDim.x) {
@@ -269,16 +289,29 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
             for (int k = 1; k < N; ++k) most = larger(most, y[k]);
             a.template add<N>(y, most, c);
             if (f.top) {
-                float limit = best.threshold();
-                if (__ballot(!(most < limit))) {        // rarely, once the list is full of large ones
+                // If every wave has seen `share` logits that reach a rank, the row has `top` that do: nothing below it is looked at.  At first the
+                // lanes' maxima give that rank.  (Without it each wave's own list is the only measure: 8,191 x 32,768 bf16, 20
+                // alternatives, LISTS_ALONE us.)
+                if (v0 == begin) {
+                    const uint32_t seen = wave_kth(rank_of(most), share);
+                    if (lane == 0) shared_floor[wave] = seen;
+                    __syncthreads();
+                }
+                uint32_t floor = shared_floor[0];
+#pragma unroll
+                for (int w = 1; w < LONG_WAVES; ++w) floor = min(floor, shared_floor[w]);
+                float limit = threshold(max(floor, (uint32_t)(best.limit >> 32)));
+                if (__ballot(!(most < limit))) {
 #pragma unroll
                     for (int k = N - 1; k >= 0; --k) {
                         const bool near = !(y[k] < limit);
                         if (!__ballot(near)) continue;
                         const int64_t p = v + (k / W) * LONG_THREADS, j = p * W + k % W - before;
                         best.insert(near && p < end && j >= 0 && j < f.classes ? key_of(y[k], (uint32_t)j) : 0, f.top);
-                        limit = best.threshold();
+                        limit = threshold(max(floor, (uint32_t)(best.limit >> 32)));
                     }
+                    const uint32_t seen = (uint32_t)(read_lane(best.key, share - 1) >> 32);
+                    if (lane == 0 && seen > shared_floor[wave]) shared_floor[wave] = seen;
                 }
             }
 #pragma unroll
@@ -349,17 +382,21 @@ struct RowGradient {
     float m, logs, a, b, d;
     int64_t target;
     bool empty;
-    __device__ RowGradient(const Backward &g, int64_t i) {
+    // L lanes, which all come here, for a row; the rows' lanes share the alternatives
+    template <int L> __device__ void load(const Backward &g, int64_t i, int lane) {
+        const float e = g.d_entropy ? g.d_entropy[i] : 0.f, h = g.entropy[i], given = g.d_target ? g.d_target[i] : 0.f;
+        float all = 0.f;
+        if (g.d_top) {
+            for (int k = lane; k < g.top; k += L) all += g.d_top[i * g.top + k];
+            all = over_group<L>(all, [](float x, float y) { return x + y; });
+        }
         m = g.stats[2 * i];
         logs = g.stats[2 * i + 1];
         empty = m == -INF;
         target = g.targets ? index_at(g.targets, g.index_type, i) : -1;
-        d = target == -1 || !g.d_target ? 0.f : target >= 0 && target < g.classes ? g.d_target[i] : __builtin_nanf("");
-        float all = d;
-        if (g.d_top)
-            for (int k = 0; k < g.top; ++k) all += g.d_top[i * g.top + k];
-        const float e = g.d_entropy ? g.d_entropy[i] : 0.f;
-        a = -g.scale * fmaf(e, g.entropy[i], all);
+        d = target == -1 ? 0.f : target >= 0 && target < g.classes ? given : __builtin_nanf("");
+        if (!g.d_target) d = 0.f;
+        a = -g.scale * fmaf(e, h, d + all);
         b = -g.scale * e;
     }
     __device__ float at(float x, float scale) const {
@@ -373,11 +410,11 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
     const int lane = threadIdx.x % L;
     constexpr int EACH = 256 / L;
     for (int64_t base = (int64_t)blockIdx.x * EACH; base < g.n; base += (int64_t)gridDim.x * EACH) {
-        const int64_t i = base + threadIdx.x / L;
-        if (i >= g.n) return;
+        const int64_t i = min(base + threadIdx.x / L, g.n - 1);         // (rows behind the last one: the last one once more)
         Row row;
         row.load(logits + i * g.ld, (int)g.classes, lane, whole, true);
-        const RowGradient r(g, i);
+        RowGradient r;
+        r.template load<L>(g, i, lane);
         T *o = out + i * g.ld_out;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -409,42 +446,69 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
 // taken from the last to the first: the forward pass has just read the last ones.
 template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
     constexpr int W = VECTOR<T>, U = 32 / W;
+    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
     for (int64_t unit = (int64_t)blockIdx.x; unit < g.n * runs; unit += gridDim.x) {
         const int64_t i = g.n - 1 - unit / runs, run = unit % runs;
         const T *x = logits + i * g.ld;
         T *o = out + i * g.ld_out;
-        const RowGradient r(g, i);
         const int before = (int)((uintptr_t)x % 16 / sizeof(T));
-        const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
-        const int64_t first = run * (U * LONG_THREADS);
+        const int64_t first = run * (U * LONG_THREADS), low = first * W - before, high = low + (int64_t)U * LONG_THREADS * W;
+        RowGradient r;
+        if ((uintptr_t)o % 16 == (uintptr_t)x % 16 && low >= 0 && high <= g.classes) {
+            uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t j = (first + u * LONG_THREADS + threadIdx.x) * W - before;
-            float y[W];
-            if (alike && j >= 0 && j + W <= g.classes) {
-                unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
+            for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + low + (u * LONG_THREADS + threadIdx.x) * W);
+            r.load<WAVE_LANES>(g, i, lane);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float y[W];
+                unpack<T>(raw[u], y);
 #pragma unroll
                 for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
-                *reinterpret_cast<uint4 *>(o + j) = pack<T>(y);
-            } else {
+                *reinterpret_cast<uint4 *>(o + low + (u * LONG_THREADS + threadIdx.x) * W) = pack<T>(y);
+            }
+        } else {
+            const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
+            r.load<WAVE_LANES>(g, i, lane);
 #pragma unroll
-                for (int k = 0; k < W; ++k)
-                    if (j + k >= 0 && j + k < g.classes) o[j + k] = round_to<T>(r.at(load_as_float(x[j + k]), g.scale));
+            for (int u = 0; u < U; ++u) {
+                const int64_t j = low + (u * LONG_THREADS + threadIdx.x) * W;
+                float y[W];
+                if (alike && j >= 0 && j + W <= g.classes) {
+                    unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
+#pragma unroll
+                    for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
+                    *reinterpret_cast<uint4 *>(o + j) = pack<T>(y);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < W; ++k)
+                        if (j + k >= 0 && j + k < g.classes) o[j + k] = round_to<T>(r.at(load_as_float(x[j + k]), g.scale));
+                }
             }
         }
         if (r.empty || (r.target < 0 && !g.d_top)) continue;        // the same for the whole workgroup
         __syncthreads();
-        const int64_t low = first * W - before, high = low + (int64_t)U * LONG_THREADS * W;
-        const int k = threadIdx.x;
-        if (k <= (g.d_top ? g.top : 0)) {
-            const int64_t j = k ? g.top_index[i * g.top + k - 1] : r.target;
-            if (j >= 0 && j >= low && j < high && j < g.classes) {
-                float more = j == r.target ? r.d : 0.f;
+        // The first wave writes the alternatives, the second one the target unless it is among them.  (An index that comes twice gets both.)
+        if (wave < 2) {
+            const bool listed = g.d_top && lane < g.top;
+            int64_t j = listed ? g.top_index[i * g.top + lane] : -1;
+            float more = listed ? g.d_top[i * g.top + lane] : 0.f;
+            if (wave == 0) {
+                const float mine = more;
                 if (g.d_top)
-                    for (int a = 0; a < g.top; ++a)
-                        if (g.top_index[i * g.top + a] == j) more += g.d_top[i * g.top + a];
-                o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
+                    for (int a = 1; a < g.top; ++a) {
+                        const int other = (lane + a) % g.top;
+                        const int64_t k = (int64_t)__shfl((long long)j, other);
+                        const float d = __shfl(mine, other);
+                        if (listed && k == j) more += d;
+                    }
+                if (listed && j == r.target) more += r.d;
+            } else {
+                const bool among = __ballot(listed && j == r.target) != 0;
+                j = lane == 0 && !among ? r.target : -1;
+                more = r.d;
             }
+            if (j >= 0 && j >= low && j < high && j < g.classes) o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
         }
         __syncthreads();
     }
