@@ -22,7 +22,8 @@ constexpr int64_t LAUNCH_BLOCKS = 1 << 22;      // the threads of a launch are c
 struct Tensors {                    // of one launch, in its arguments: nothing is copied to the device beforehand
     libra_adamw_tensor_t t[LAUNCH_TENSORS];
     int32_t first[LAUNCH_TENSORS];  // workgroup that each begins with
-    int64_t begin[LAUNCH_TENSORS];  // and the block of the tensor that this workgroup takes
+    int64_t begin[LAUNCH_TENSORS];  // and the workgroup of the tensor that this one is
+    bool aligned[LAUNCH_TENSORS];   // every array to 16 bytes
     int32_t count;
 };
 
@@ -95,66 +96,116 @@ __device__ inline Element updated(const Step &s, float p, float g, float m, floa
     return e;
 }
 
-// a workgroup per 256 elements
+// N neighbouring numbers from `i` on, in 16-byte pieces if `whole`; those from `n` on are zeros, and are not written
+template <class T, int N> struct Run {
+    T x[N];
+    __device__ void load(const T *p, int64_t i, int64_t n, bool whole) {
+        constexpr int BYTES = N * (int)sizeof(T);
+        if (whole) {
+            if constexpr (BYTES >= 16) {
+#pragma unroll
+                for (int k = 0; k < BYTES / 16; ++k) reinterpret_cast<uint4 *>(x)[k] = reinterpret_cast<const uint4 *>(p + i)[k];
+            } else *reinterpret_cast<uint2 *>(x) = *reinterpret_cast<const uint2 *>(p + i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = i + k < n ? p[i + k] : T(0);
+        }
+    }
+    __device__ void store(T *p, int64_t i, int64_t n, bool whole) const {
+        constexpr int BYTES = N * (int)sizeof(T);
+        if (whole) {
+            if constexpr (BYTES >= 16) {
+#pragma unroll
+                for (int k = 0; k < BYTES / 16; ++k) reinterpret_cast<uint4 *>(p + i)[k] = reinterpret_cast<const uint4 *>(x)[k];
+            } else *reinterpret_cast<uint2 *>(p + i) = *reinterpret_cast<const uint2 *>(x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (i + k < n) p[i + k] = x[k];
+        }
+    }
+};
+
+// A workgroup takes eight blocks of 256 elements, a thread eight neighbouring elements: 32 lanes have a block of 8-bit states.
+constexpr int EACH = 8, GROUP_BLOCKS = 256 * EACH / STATE_BLOCK, BLOCK_LANES = STATE_BLOCK / EACH;
+
 template <class T, bool BITS8>
 __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
-    __shared__ uint32_t most[2][4];
     read_step(s);
     int k = 0;
     while (k + 1 < list.count && list.first[k + 1] <= (int)blockIdx.x) ++k;
-    const libra_adamw_tensor_t t = list.t[k];
-    const int64_t block = list.begin[k] + (blockIdx.x - list.first[k]), i = block * STATE_BLOCK + threadIdx.x;
-    const bool real = i < t.n;
-    float p = 0.f, g = 0.f, m = 0.f, v = 0.f, r;
-    if (real) {
-        p = t.master ? t.master[i] : load_as_float(((T *)t.param)[i]);
-        g = load_as_float(((const T *)t.grad)[i]);
-        if (BITS8) {
-            m = e4m3_value(((uint8_t *)t.first)[i]) * t.first_scales[block];
-            r = e4m3_value(((uint8_t *)t.second)[i]) * t.second_scales[block];
-            v = r * r;
-        } else {
-            m = ((float *)t.first)[i];
-            v = ((float *)t.second)[i];
-        }
-    }
-    const Element e = updated(s, p, g, m, v, r);
-    if (real) {
-        if (t.master) t.master[i] = e.p;
-        ((T *)t.param)[i] = round_to<T>(e.p);
-    }
-    if (!BITS8) {
-        if (real) {
-            ((float *)t.first)[i] = e.m;
-            ((float *)t.second)[i] = e.v;
-        }
-        return;
-    }
+    const libra_adamw_tensor_t &t = list.t[k];
+    const int64_t i = (list.begin[k] + (blockIdx.x - list.first[k])) * (GROUP_BLOCKS * STATE_BLOCK) + threadIdx.x * EACH, n = t.n;
+    const bool whole = list.aligned[k] && i + EACH <= n;
+    const int64_t block = min(i, n - 1) / STATE_BLOCK;
+    Run<T, EACH> p, g;
+    Run<float, EACH> w, m, v;
+    Run<uint8_t, EACH> first, second;
     float scale[2];
-    const float x[2] = {e.m, r};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        uint32_t a = __float_as_uint(fabsf(x[j]));
-        if (!real || a >= 0x7f800000u) a = 0;
-        for (int d = 32; d; d /= 2) a = max(a, (uint32_t)__shfl_xor((int)a, d));
-        if (threadIdx.x % 64 == 0) most[j][threadIdx.x / 64] = a;
+    g.load((const T *)t.grad, i, n, whole);
+    if (t.master) w.load(t.master, i, n, whole);
+    else p.load((const T *)t.param, i, n, whole);
+    if constexpr (BITS8) {
+        first.load((const uint8_t *)t.first, i, n, whole);
+        second.load((const uint8_t *)t.second, i, n, whole);
+        scale[0] = t.first_scales[block];
+        scale[1] = t.second_scales[block];
+    } else {
+        m.load((const float *)t.first, i, n, whole);
+        v.load((const float *)t.second, i, n, whole);
     }
-    __syncthreads();
+    if (!t.master)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t a = max(max(most[j][0], most[j][1]), max(most[j][2], most[j][3]));
-        const int ex = max((int)(a >> 23) - 135 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0), -126);
-        scale[j] = __uint_as_float((uint32_t)(ex + 127) << 23);
+        for (int e = 0; e < EACH; ++e) w.x[e] = load_as_float(p.x[e]);
+    float r[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        if constexpr (BITS8) {
+            m.x[e] = e4m3_value(first.x[e]) * scale[0];
+            const float root = e4m3_value(second.x[e]) * scale[1];
+            v.x[e] = root * root;
+        }
+        const Element u = updated(s, w.x[e], load_as_float(g.x[e]), m.x[e], v.x[e], r[e]);
+        w.x[e] = u.p;
+        m.x[e] = u.m;
+        v.x[e] = u.v;
+        p.x[e] = round_to<T>(u.p);
     }
-    if (!real) return;
-    const uint32_t key = mix(mix(mix(s.seed) + s.step) + t.number), h = mix(key + (uint32_t)i + (uint32_t)(i >> 32) * 0x9E3779B1u);
-    const float chance[2] = {(float)(h & 0xffff) * 0x1p-16f, (float)(h >> 16) * 0x1p-16f};
-    const uint32_t sign = __float_as_uint(e.m) >> 31 << 7;
-    ((uint8_t *)t.first)[i] = (uint8_t)(e4m3_code(e.m, 1.f / scale[0], chance[0], false) | sign);
-    ((uint8_t *)t.second)[i] = (uint8_t)e4m3_code(r, 1.f / scale[1], chance[1], true);
-    if (threadIdx.x == 0) {
-        t.first_scales[block] = scale[0];
-        t.second_scales[block] = scale[1];
+    p.store((T *)t.param, i, n, whole);
+    if (t.master) w.store(t.master, i, n, whole);
+    if constexpr (!BITS8) {
+        m.store((float *)t.first, i, n, whole);
+        v.store((float *)t.second, i, n, whole);
+    } else {
+        const uint32_t key = mix(mix(mix(s.seed) + s.step) + t.number);
+        uint32_t most[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {            // (what lies behind the end is zero)
+            const uint32_t a = __float_as_uint(fabsf(m.x[e])), b = __float_as_uint(r[e]);
+            most[0] = max(most[0], a < 0x7f800000u ? a : 0);
+            most[1] = max(most[1], b < 0x7f800000u ? b : 0);
+        }
+        float inverse[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t a = over_group<BLOCK_LANES>(most[j], [](uint32_t x, uint32_t y) { return max(x, y); });
+            const int ex = max((int)(a >> 23) - 135 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0), -126);
+            scale[j] = __uint_as_float((uint32_t)(127 + ex) << 23);
+            inverse[j] = __uint_as_float((uint32_t)(127 - ex) << 23);
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const uint32_t h = mix(key + (uint32_t)(i + e) + (uint32_t)((i + e) >> 32) * 0x9E3779B1u);
+            const float chance[2] = {(float)(h & 0xffff) * 0x1p-16f, (float)(h >> 16) * 0x1p-16f};
+            first.x[e] = (uint8_t)(e4m3_code(m.x[e], inverse[0], chance[0], false) | __float_as_uint(m.x[e]) >> 31 << 7);
+            second.x[e] = (uint8_t)e4m3_code(r[e], inverse[1], chance[1], true);
+        }
+        first.store((uint8_t *)t.first, i, n, whole);
+        second.store((uint8_t *)t.second, i, n, whole);
+        if (threadIdx.x % BLOCK_LANES == 0 && i < n) {
+            t.first_scales[block] = scale[0];
+            t.second_scales[block] = scale[1];
+        }
     }
 }
 
@@ -221,12 +272,16 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
         };
         for (int32_t k = 0; k < count; ++k) {
             if (tensors[k].dtype != dtype || tensors[k].n == 0) continue;
-            const int64_t all = (tensors[k].n + STATE_BLOCK - 1) / STATE_BLOCK;
+            const libra_adamw_tensor_t &t = tensors[k];
+            const bool aligned = aligned_to(t.param, 16) && aligned_to(t.grad, 16) && aligned_to(t.master, 16) && aligned_to(t.first, bits8 ? 8 : 16) &&
+                                 aligned_to(t.second, bits8 ? 8 : 16);
+            const int64_t all = (t.n + GROUP_BLOCKS * STATE_BLOCK - 1) / (GROUP_BLOCKS * STATE_BLOCK);
             for (int64_t begin = 0; begin < all;) {
                 if (list.count == LAUNCH_TENSORS || blocks == LAUNCH_BLOCKS)
                     if (int rc = launch()) return rc;
                 const int64_t some = std::min(all - begin, LAUNCH_BLOCKS - blocks);
-                list.t[list.count] = tensors[k];
+                list.t[list.count] = t;
+                list.aligned[list.count] = aligned;
                 list.first[list.count] = (int32_t)blocks;
                 list.begin[list.count++] = begin;
                 blocks += some;
