@@ -65,20 +65,22 @@ __device__ inline void read_step(Step &s) {
     s.step = number;
 }
 
-__device__ inline float e4m3_value(uint8_t code) {
-    const uint32_t e = (code >> 3) & 15, f = code & 7;
-    const float a = (code & 127) == 127 ? __builtin_nanf("") : e ? __uint_as_float((e + 120) << 23 | f << 20) : (float)f * 0x1p-9f;
-    return code & 128 ? -a : a;
+// Four e4m3 numbers
+__device__ inline void e4m3_values(uint32_t codes, float *x) {
+    const auto low = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), high = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    x[0] = low[0];
+    x[1] = low[1];
+    x[2] = high[0];
+    x[3] = high[1];
 }
 
-// |x| / scale, 0 .. 448, to one of its two neighbours; `inverse` is the power of two 1 / scale
-__device__ inline uint32_t e4m3_code(float x, float inverse, float chance, bool root) {
+// |x| / scale, 0 .. 448, to one of its two neighbours; `inverse` is the power of two 1 / scale, the chance is c / 2^16.  From 2^-6 on, where
+// a number has four digits, the chance is added below the last of them and what is carried is kept; below 2^-6 the steps are all 2^-9.
+__device__ inline uint32_t e4m3_code(float x, float inverse, uint32_t c) {
     const float y = fabsf(x) * inverse;
-    if (!(y <= 448.f)) return 127;                                       // Inf and NaN
-    const int e = max((int)(__float_as_uint(y) >> 23) - 127, -6);
-    uint32_t q = (uint32_t)(y * __uint_as_float((uint32_t)(130 - e) << 23) + chance);
-    if (root && q == 0 && x > 0.f) q = 1;
-    return (uint32_t)(e + 6) * 8 + q;
+    uint32_t code = ((__float_as_uint(y) + (c << 4)) >> 20) - (120u << 3);
+    if (y < 0x1p-6f) code = (uint32_t)(y * 0x1p9f + (float)c * 0x1p-16f);
+    return code;
 }
 
 struct Element {
@@ -92,7 +94,10 @@ __device__ inline Element updated(const Step &s, float p, float g, float m, floa
     e.m = s.b1 * m + s.c1 * g;
     e.v = s.b2 * v + s.c2 * (g * g);
     r = sqrtf(e.v);
-    e.p = s.keep * p - s.size * (e.m / (s.root * r + s.eps));
+    const float den = s.root * r + s.eps;
+    // (the quotient goes into the parameter alone: a reciprocal of one unit in the last place will do, but for numbers it flushes to zero)
+    const float q = den > 0x1p-100f && den < 0x1p100f ? e.m * __builtin_amdgcn_rcpf(den) : e.m / den;
+    e.p = s.keep * p - s.size * q;
     return e;
 }
 
@@ -126,6 +131,18 @@ template <class T, int N> struct Run {
     }
 };
 
+// Codes of N elements
+template <int N> __device__ inline void load_codes(Run<uint32_t, N / 4> &r, const uint8_t *p, int64_t i, int64_t n, bool whole) {
+    Run<uint8_t, N> bytes;
+    bytes.load(p, i, n, whole);
+    __builtin_memcpy(r.x, bytes.x, N);
+}
+template <int N> __device__ inline void store_codes(const Run<uint32_t, N / 4> &r, uint8_t *p, int64_t i, int64_t n, bool whole) {
+    Run<uint8_t, N> bytes;
+    __builtin_memcpy(bytes.x, r.x, N);
+    bytes.store(p, i, n, whole);
+}
+
 // A workgroup takes eight blocks of 256 elements, a thread eight neighbouring elements: 32 lanes have a block of 8-bit states.
 constexpr int EACH = 8, GROUP_BLOCKS = 256 * EACH / STATE_BLOCK, BLOCK_LANES = STATE_BLOCK / EACH;
 
@@ -140,14 +157,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
     const int64_t block = min(i, n - 1) / STATE_BLOCK;
     Run<T, EACH> p, g;
     Run<float, EACH> w, m, v;
-    Run<uint8_t, EACH> first, second;
+    Run<uint32_t, EACH / 4> first, second;          // four codes each
     float scale[2];
     g.load((const T *)t.grad, i, n, whole);
     if (t.master) w.load(t.master, i, n, whole);
     else p.load((const T *)t.param, i, n, whole);
     if constexpr (BITS8) {
-        first.load((const uint8_t *)t.first, i, n, whole);
-        second.load((const uint8_t *)t.second, i, n, whole);
+        load_codes<EACH>(first, (const uint8_t *)t.first, i, n, whole);
+        load_codes<EACH>(second, (const uint8_t *)t.second, i, n, whole);
         scale[0] = t.first_scales[block];
         scale[1] = t.second_scales[block];
     } else {
@@ -158,12 +175,19 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) w.x[e] = load_as_float(p.x[e]);
     float r[EACH];
+    if constexpr (BITS8) {
+#pragma unroll
+        for (int e = 0; e < EACH; e += 4) {
+            e4m3_values(first.x[e / 4], m.x + e);
+            e4m3_values(second.x[e / 4], v.x + e);
+        }
+    }
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
         if constexpr (BITS8) {
-            m.x[e] = e4m3_value(first.x[e]) * scale[0];
-            const float root = e4m3_value(second.x[e]) * scale[1];
-            v.x[e] = root * root;
+            m.x[e] *= scale[0];
+            v.x[e] *= scale[1];
+            v.x[e] *= v.x[e];
         }
         const Element u = updated(s, w.x[e], load_as_float(g.x[e]), m.x[e], v.x[e], r[e]);
         w.x[e] = u.p;
@@ -181,9 +205,18 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
         uint32_t most[2] = {0, 0};
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {            // (what lies behind the end is zero)
-            const uint32_t a = __float_as_uint(fabsf(m.x[e])), b = __float_as_uint(r[e]);
-            most[0] = max(most[0], a < 0x7f800000u ? a : 0);
-            most[1] = max(most[1], b < 0x7f800000u ? b : 0);
+            most[0] = max(most[0], __float_as_uint(fabsf(m.x[e])));
+            most[1] = max(most[1], __float_as_uint(r[e]) & 0x7fffffffu);
+        }
+        const bool odd = __ballot(max(most[0], most[1]) >= 0x7f800000u) != 0;       // an Inf or NaN in this wave
+        if (odd) {
+            most[0] = most[1] = 0;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const uint32_t a = __float_as_uint(fabsf(m.x[e])), b = __float_as_uint(r[e]) & 0x7fffffffu;
+                most[0] = max(most[0], a < 0x7f800000u ? a : 0);
+                most[1] = max(most[1], b < 0x7f800000u ? b : 0);
+            }
         }
         float inverse[2];
 #pragma unroll
@@ -193,15 +226,27 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
             scale[j] = __uint_as_float((uint32_t)(127 + ex) << 23);
             inverse[j] = __uint_as_float((uint32_t)(127 - ex) << 23);
         }
+        const uint32_t place = key + (uint32_t)i + (uint32_t)(i >> 32) * 0x9E3779B1u;      // (eight neighbours have one high word)
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const uint32_t h = mix(key + (uint32_t)(i + e) + (uint32_t)((i + e) >> 32) * 0x9E3779B1u);
-            const float chance[2] = {(float)(h & 0xffff) * 0x1p-16f, (float)(h >> 16) * 0x1p-16f};
-            first.x[e] = (uint8_t)(e4m3_code(m.x[e], inverse[0], chance[0], false) | __float_as_uint(m.x[e]) >> 31 << 7);
-            second.x[e] = (uint8_t)e4m3_code(r[e], inverse[1], chance[1], true);
+        for (int q = 0; q < EACH / 4; ++q) {
+            uint32_t one = 0, two = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = 4 * q + k;
+                const uint32_t h = mix(place + e);
+                uint32_t a = e4m3_code(m.x[e], inverse[0], h & 0xffff), b = max(e4m3_code(r[e], inverse[1], h >> 16), min(__float_as_uint(r[e]), 1u));
+                if (odd) {
+                    if (!(fabsf(m.x[e]) < INFINITY)) a = 127;
+                    if (!(r[e] < INFINITY)) b = 127;
+                }
+                one |= (a | __float_as_uint(m.x[e]) >> 31 << 7) << (8 * k);
+                two |= b << (8 * k);
+            }
+            first.x[q] = one;
+            second.x[q] = two;
         }
-        first.store((uint8_t *)t.first, i, n, whole);
-        second.store((uint8_t *)t.second, i, n, whole);
+        store_codes<EACH>(first, (uint8_t *)t.first, i, n, whole);
+        store_codes<EACH>(second, (uint8_t *)t.second, i, n, whole);
         if (threadIdx.x % BLOCK_LANES == 0 && i < n) {
             t.first_scales[block] = scale[0];
             t.second_scales[block] = scale[1];
