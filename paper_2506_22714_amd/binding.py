@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -821,9 +822,10 @@ def _code(t, name: str) -> int:
 def _rows_of(t, name: str, cols=None, like=None) -> int:
     """A matrix whose rows are contiguous (with any distance between them); its type's code."""
     code = _code(t, name)
-    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ('*', {'*' if cols is None else cols})")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    shape = t.shape
+    if len(shape) != 2 or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected ('*', {'*' if cols is None else cols})")
+    if not t.is_contiguous() and (shape[1] > 1 and t.stride(1) != 1 or shape[0] > 1 and t.stride(0) < shape[1]):
         raise ValueError(f"{name}: rows must be contiguous (strides {tuple(t.stride())})")
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a GPU tensor")
@@ -833,7 +835,7 @@ def _rows_of(t, name: str, cols=None, like=None) -> int:
 
 
 def _ld(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.shape[1] if t.is_contiguous() or t.shape[0] <= 1 else t.stride(0)
 
 
 def _index_code(t, name: str, like) -> int:
@@ -864,16 +866,15 @@ def embedding(table, index, scale: float = 1.0, out=None):
     if width < 1:
         raise ValueError("table: rows of no elements")
     if out is None:
-        out = torch.empty((n, width), dtype=table.dtype, device=table.device)
-        result = out.view(*index.shape, width)
+        out, ld_out = torch.empty((*index.shape, width), dtype=table.dtype, device=table.device), width
     else:
         _rows_of(out, "out", width, like=table)
         if out.shape[0] != n:
             raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
-        result = out
+        ld_out = _ld(out)
     _launch(lib().libra_embedding, "libra_embedding", table, table.data_ptr(), rows, width, _ld(table), dtype, index.data_ptr(), kind, n, scale,
-            out.data_ptr(), _ld(out))
-    return result
+            out.data_ptr(), ld_out)
+    return out
 
 
 def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
@@ -965,11 +966,14 @@ def log_probs_backward(logits, result: LogProbs, targets=None, d_target=None, d_
     return out
 
 
-def _adamw_array(t, name: str, k: int, dtype, n: int, device: int) -> int:
-    if not isinstance(t, _torch.Tensor) or t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
-        what = f"{t.dtype}, {t.numel()} elements, contiguous: {t.is_contiguous()}, {t.device}" if isinstance(t, _torch.Tensor) else type(t).__name__
-        raise ValueError(f"{name}[{k}]: {what}; expected contiguous {dtype} of {n} elements on GPU {device}")
-    return t.data_ptr()
+def _adamw_refuse(k: int, arrays, dtype, n: int, device: int):
+    """Says which of the arrays of parameter k is not what it should be: (name, tensor, type, elements) each."""
+    for name, t, want, many in arrays:
+        if not isinstance(t, _torch.Tensor):
+            raise ValueError(f"{name}[{k}]: expected a torch tensor, got {type(t).__name__}")
+        if t.dtype is not want or t.numel() != many or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"{name}[{k}]: {t.dtype}, {t.numel()} elements, contiguous: {t.is_contiguous()}, {t.device}; expected contiguous "
+                             f"{want} of {many} elements on GPU {device}")
 
 
 def _one_on(x, name: str, dtype, like) -> int:
@@ -1003,26 +1007,40 @@ def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: 
     device = params[0].get_device()
     if device < 0:
         raise ValueError("params[0]: must be a GPU tensor")
-    table = (AdamwTensor * count)()
-    seen = set()
+    float32 = torch.float32
+    codes = {torch.float16: F16, torch.bfloat16: BF16, float32: F32}
+    fields, seen = [], set()            # a record of AdamwTensor is eight words and two halves of one
     for k, p in enumerate(params):
-        code, n = _code(p, f"params[{k}]"), p.numel()
-        r = table[k]
-        r.param = _adamw_array(p, "params", k, p.dtype, n, device)
-        r.grad = _adamw_array(grads[k], "grads", k, p.dtype, n, device)
-        r.first = _adamw_array(first[k], "first", k, state, n, device)
-        r.second = _adamw_array(second[k], "second", k, state, n, device)
-        if bits8:
+        g, m, v = grads[k], first[k], second[k]
+        ms, vs = (first_scales[k], second_scales[k]) if bits8 else (None, None)
+        w = masters[k] if masters is not None else None
+        try:
+            dtype, n = p.dtype, p.numel()
             blocks = -(-n // ADAMW_BLOCK)
-            r.first_scales = _adamw_array(first_scales[k], "first_scales", k, torch.float32, blocks, device)
-            r.second_scales = _adamw_array(second_scales[k], "second_scales", k, torch.float32, blocks, device)
-        if masters is not None and masters[k] is not None:
-            r.master = _adamw_array(masters[k], "masters", k, torch.float32, n, device)
-        r.n, r.dtype, r.number = n, code, k if numbers is None else numbers[k]
+            fine = (dtype in codes and p.is_contiguous() and p.get_device() == device
+                    and g.dtype is dtype and g.numel() == n and g.is_contiguous() and g.get_device() == device
+                    and m.dtype is state and m.numel() == n and m.is_contiguous() and m.get_device() == device
+                    and v.dtype is state and v.numel() == n and v.is_contiguous() and v.get_device() == device
+                    and (w is None or w.dtype is float32 and w.numel() == n and w.is_contiguous() and w.get_device() == device)
+                    and (not bits8 or ms.dtype is float32 and ms.numel() == blocks and ms.is_contiguous() and ms.get_device() == device
+                         and vs.dtype is float32 and vs.numel() == blocks and vs.is_contiguous() and vs.get_device() == device))
+        except AttributeError:
+            fine = False
+        if not fine:
+            _code(p, f"params[{k}]")
+            n = p.numel()
+            more = [("first_scales", ms, float32, -(-n // ADAMW_BLOCK)), ("second_scales", vs, float32, -(-n // ADAMW_BLOCK))] if bits8 else []
+            _adamw_refuse(k, [("params", p, p.dtype, n), ("grads", g, p.dtype, n), ("first", m, state, n), ("second", v, state, n), *more,
+                              *([("masters", w, float32, n)] if w is not None else [])], p.dtype, n, device)
+        at = p.data_ptr()
         if n:
-            if r.param in seen:
+            if at in seen:
                 raise ValueError(f"params[{k}]: the same tensor twice")
-            seen.add(r.param)
+            seen.add(at)
+        number = k if numbers is None else numbers[k] & 0xffffffff
+        fields += (at, g.data_ptr(), m.data_ptr(), v.data_ptr(), ms.data_ptr() if bits8 else 0, vs.data_ptr() if bits8 else 0,
+                   w.data_ptr() if w is not None else 0, n, codes[dtype] | number << 32)
+    table = struct.pack(f"{len(fields)}Q", *fields)
     opts = AdamwOpts(state_bits=8 if bits8 else 32, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=seed & 0xffffffff)
     if isinstance(step, torch.Tensor):
         opts.step_dev = _one_on(step, "step", torch.int64, params[0])

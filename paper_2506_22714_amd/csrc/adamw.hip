@@ -149,8 +149,9 @@ constexpr int EACH = 8, GROUP_BLOCKS = 256 * EACH / STATE_BLOCK, BLOCK_LANES = S
 template <class T, bool BITS8>
 __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
     read_step(s);
-    int k = 0;
-    while (k + 1 < list.count && list.first[k + 1] <= (int)blockIdx.x) ++k;
+    int k = -1;
+#pragma unroll
+    for (int j = 0; j < LAUNCH_TENSORS; ++j) k += list.first[j] <= (int)blockIdx.x;     // (all loaded at once; behind the last tensor: none)
     const libra_adamw_tensor_t &t = list.t[k];
     const int64_t i = (list.begin[k] + (blockIdx.x - list.first[k])) * (GROUP_BLOCKS * STATE_BLOCK) + threadIdx.x * EACH, n = t.n;
     const bool whole = list.aligned[k] && i + EACH <= n;
@@ -305,6 +306,7 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
         list.count = 0;
         auto launch = [&]() {
             if (!list.count) return LIBRA_OK;
+            for (int j = list.count; j < LAUNCH_TENSORS; ++j) list.first[j] = INT32_MAX;
             const int rc = for_dtype(dtype, [&](auto tag) {
                 typedef decltype(tag) T;
                 if (bits8) hipLaunchKernelGGL((adamw_kernel<T, true>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, list, s);

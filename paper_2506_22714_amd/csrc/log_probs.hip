@@ -198,6 +198,7 @@ struct Best {
     }
 };
 
+
 // The largest rank of the wave, in a scalar register
 __device__ inline uint32_t wave_most(uint32_t x) {
     x = over_group<16>(x, [](uint32_t p, uint32_t q) { return max(p, q); });
@@ -222,8 +223,15 @@ template <class F> __device__ inline void merge_lists(const uint64_t *keys, int 
     int at = 0;
     uint64_t head = lane < lists ? keys[lane * top] : 0;
     for (int a = 0; a < top; ++a) {
-        const uint64_t best = over_group<WAVE_LANES>(head, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-        if (head == best) {                             // keys differ, but for the zeros of lists that are not full
+        const uint32_t rank = wave_most((uint32_t)(head >> 32));
+        uint64_t those = __ballot((uint32_t)(head >> 32) == rank);
+        if (those & (those - 1)) {                      // several: the lowest class, which has the largest low word
+            const uint32_t low = wave_most((uint32_t)(head >> 32) == rank ? (uint32_t)head : 0);
+            those = __ballot((uint32_t)(head >> 32) == rank && (uint32_t)head == low);
+        }
+        const int from = __ffsll((unsigned long long)those) - 1;
+        const uint64_t best = read_lane(head, from);
+        if (lane == from) {
             ++at;
             head = lane < lists && at < top ? keys[lane * top + at] : 0;
         }
