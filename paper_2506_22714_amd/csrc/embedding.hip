@@ -267,23 +267,25 @@ struct Keys {                       // of one pass: the ids themselves in the fi
     __device__ uint2 at(int64_t i) const { return pair ? pair[i] : uint2{key_at(index, index_type, rows, i), (uint32_t)i}; }
 };
 
-// What the zeros of the table are written to by the launch of the first count: workgroups behind the counting ones
+// A share of the table's zeros, written by workgroups behind those of a sorting launch: these wait for chains of loads and LDS accesses and
+// leave the memory to others (all zeros in the first launch: 143 us for 2^20 ids on 2^20 rows of 128 bytes, not SHARED).
 struct Zeros {
     char *base;
     int64_t rows, width_bytes, ld_bytes;
     unsigned blocks;
+    int share, shares;
 };
-__device__ inline void write_zeros(const Zeros &z, unsigned block) {
-    const int64_t first = (int64_t)block * SORT_THREADS + threadIdx.x, step = (int64_t)z.blocks * SORT_THREADS;
+__device__ inline void write_zeros(const Zeros &z, unsigned block, int threads) {
+    const int64_t first = (int64_t)block * threads + threadIdx.x, step = (int64_t)z.blocks * threads;
     if (z.width_bytes == z.ld_bytes && ((uintptr_t)z.base & 15) == 0) {
-        const int64_t bytes = z.rows * z.width_bytes;
+        const int64_t bytes = z.rows * z.width_bytes, all = bytes / 16, from = all / z.shares * z.share, to = z.share + 1 < z.shares ? all / z.shares * (z.share + 1) : all;
         uint4 *p = reinterpret_cast<uint4 *>(z.base);
-        for (int64_t k = first; k < bytes / 16; k += step) p[k] = uint4{0, 0, 0, 0};
-        if (first < bytes % 16) z.base[bytes / 16 * 16 + first] = 0;
+        for (int64_t k = from + first; k < to; k += step) p[k] = uint4{0, 0, 0, 0};
+        if (to == all && first < bytes % 16) z.base[all * 16 + first] = 0;
         return;
     }
-    const int64_t halves = z.width_bytes / 2;               // a wave per row
-    for (int64_t r = first / WAVE_LANES; r < z.rows; r += step / WAVE_LANES)
+    const int64_t halves = z.width_bytes / 2, from = z.rows / z.shares * z.share, to = z.share + 1 < z.shares ? z.rows / z.shares * (z.share + 1) : z.rows;
+    for (int64_t r = from + first / WAVE_LANES; r < to; r += step / WAVE_LANES)      // a wave per row
         for (int64_t k = threadIdx.x % WAVE_LANES; k < halves; k += WAVE_LANES) reinterpret_cast<uint16_t *>(z.base + r * z.ld_bytes)[k] = 0;
 }
 
@@ -291,7 +293,7 @@ __device__ inline void write_zeros(const Zeros &z, unsigned block) {
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, unsigned blocks, int32_t *count, Zeros zeros) {
     __shared__ int32_t seen[DIGITS];
     if (blockIdx.x >= blocks) {
-        write_zeros(zeros, blockIdx.x - blocks);
+        write_zeros(zeros, blockIdx.x - blocks, SORT_THREADS);
         return;
     }
     for (int d = threadIdx.x; d < DIGITS; d += SORT_THREADS) seen[d] = 0;
@@ -337,11 +339,15 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(int32_t *count, int blo
 
 // A tile of 4,096 pairs at a time: their numbers among the tile's pairs of the same digit, wave by wave, and from there their places.
 // Many waves of few pairs: ranking is a chain of ballots and LDS accesses (four waves of 16 pairs a lane took 15 us for a tile, not 7).
-__global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, const int32_t *count, const int32_t *totals, uint2 *out) {
+__global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int64_t n, int64_t each, int shift, int bits, unsigned blocks, const int32_t *count, const int32_t *totals, uint2 *out, Zeros zeros) {
     __shared__ int32_t next[DIGITS], part[PLACE_WAVES];
     __shared__ uint16_t mine[PLACE_WAVES][DIGITS];               // pairs of each wave, then of the waves before it: below 4,096
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES, digits = 1 << bits;
     constexpr int EACH = DIGITS / PLACE_THREADS;
+    if (blockIdx.x >= blocks) {
+        write_zeros(zeros, blockIdx.x - blocks, PLACE_THREADS);
+        return;
+    }
     {   // where this block's first pair of each digit goes: totals of the digits before, and what earlier blocks have
         int32_t t[EACH], earlier[EACH], sum = 0;
 #pragma unroll
@@ -353,7 +359,7 @@ __global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int6
                 earlier[k] = count[(int64_t)blockIdx.x * DIGITS + d];
             } else if (d < digits) {
 #pragma unroll 8
-                for (int b = 0; b < (int)gridDim.x; ++b) {
+                for (int b = 0; b < (int)blocks; ++b) {
                     const int32_t x = count[(int64_t)b * DIGITS + d];
                     t[k] += x;
                     earlier[k] += b < (int)blockIdx.x ? x : 0;
@@ -464,26 +470,28 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld
     leave(end == n || pair[end].x != row);
 }
 
-// Rows of several runs.  A workgroup looks at 64 runs and adds up the rows that begin in one of them and go on behind it: a group of lanes
-// each, which walks on while runs begin with the row; all groups together those that reach over more than 32 runs.
-constexpr int JOIN_RUNS = 64, LONG_JOIN = 32;
+// Rows of several runs.  A workgroup looks at as many runs as it has groups of lanes (16 at least) and adds up the rows that begin in one of
+// them and go on behind it: a group each, which walks on while runs begin with the row; all groups together those that reach over more
+// than 32 runs.
+constexpr int LONG_JOIN = 32;
+__host__ __device__ constexpr int join_runs(int lanes) { return 256 / lanes < 16 ? 16 : 256 / lanes < WAVE_LANES ? 256 / lanes : WAVE_LANES; }
 
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(256) void join_runs_kernel(const uint2 *pair, int64_t n, int32_t run, int64_t runs, int64_t rows, int32_t width, float scale, T *dtable,
                                                         int64_t ld_dtable, const float *part, int32_t part_width, int lanes) {
     typedef Piece<T, WHOLE> P;
     constexpr int U = 4;
-    __shared__ int64_t head[JOIN_RUNS];                         // row; as ~row if it is a long one; 2^40 for none
+    __shared__ int64_t head[WAVE_LANES];                        // row; as ~row if it is a long one; 2^40 for none
     __shared__ float shared[256 * P::W];
     __shared__ uint64_t shorts, longs;                          // which of the runs
     __shared__ unsigned equal;
-    static_assert(JOIN_RUNS == WAVE_LANES, "a wave looks at them");
     constexpr int64_t NONE = 1ll << 40;
-    const int64_t first = (int64_t)blockIdx.x * JOIN_RUNS;
-    if (threadIdx.x < JOIN_RUNS) {
+    const int many = join_runs(lanes);
+    const int64_t first = (int64_t)blockIdx.x * many;
+    if (threadIdx.x < WAVE_LANES) {
         const int64_t k = first + threadIdx.x;
         int64_t h = NONE;
-        if (k + 1 < runs) {
+        if ((int)threadIdx.x < many && k + 1 < runs) {
             const int64_t beyond = min(k + 1 + LONG_JOIN, runs - 1);
             const uint32_t row = pair[(k + 1) * run].x, end = pair[(k + 1) * run - 1].x, begin = pair[k * run].x, before = pair[max(k * run - 1, (int64_t)0)].x, far = pair[beyond * run].x;
             if (row < (uint32_t)rows && end == row && (begin != row || before != row || k == 0)) h = far == row && beyond == k + 1 + LONG_JOIN ? ~(int64_t)row : (int64_t)row;
@@ -503,7 +511,7 @@ __global__ __launch_bounds__(256) void join_runs_kernel(const uint2 *pair, int64
         return p;
     };
     if (there)
-        for (int h = group; h < JOIN_RUNS; h += groups) {
+        for (int h = group; h < many; h += groups) {
             if (!(shorts >> h & 1)) continue;
             const int64_t row = head[h];
             P sum = load(2 * (first + h) + 1);                  // what this run left for the row behind its end, and the first sums of those behind
@@ -697,10 +705,13 @@ extern "C" int libra_embedding_backward(const void *dout, int64_t ld_dout, int d
     const size_t size = dtype_bytes(dtype);
     for (int p = 0, shift = 0; p < passes; ++p) {
         const int digit = (bits - shift + passes - p - 1) / (passes - p);
-        const Zeros zeros{(char *)dtable, rows, (int64_t)width * (int64_t)size, ld_dtable * (int64_t)size, p == 0 ? 2048u : 0u};
+        Zeros zeros{(char *)dtable, rows, (int64_t)width * (int64_t)size, ld_dtable * (int64_t)size, 1024, 2 * p, 2 * passes};
         hipLaunchKernelGGL(sort_count_kernel, dim3(blocks + zeros.blocks), dim3(SORT_THREADS), 0, s, in, n, each, shift, digit, blocks, w.count, zeros);
         if (scan) hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((1 << digit) + SCAN_DIGITS - 1) / SCAN_DIGITS), dim3(1024), 0, s, w.count, (int)blocks, w.totals);
-        hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(PLACE_THREADS), 0, s, in, n, each, shift, digit, w.count, scan ? w.totals : nullptr, w.pair[p & 1]);
+        zeros.blocks = 256;
+        zeros.share = 2 * p + 1;
+        hipLaunchKernelGGL(sort_place_kernel, dim3(blocks + zeros.blocks), dim3(PLACE_THREADS), 0, s, in, n, each, shift, digit, blocks, w.count, scan ? w.totals : nullptr,
+                           w.pair[p & 1], zeros);
         in.pair = w.pair[p & 1];
         shift += digit;
     }
@@ -711,7 +722,7 @@ extern "C" int libra_embedding_backward(const void *dout, int64_t ld_dout, int d
         const int groups = 256 / l.lanes;
         hipLaunchKernelGGL((run_sums_kernel<T, WHOLE>), dim3((unsigned)((w.runs + groups - 1) / groups), l.slices), dim3(256), 0, s, (const T *)dout, ld_dout, in.pair, n, w.run, rows,
                            width, scale, (T *)dtable, ld_dtable, w.part, w.part_width, l.lanes);
-        hipLaunchKernelGGL((join_runs_kernel<T, WHOLE>), dim3((unsigned)((w.runs + JOIN_RUNS - 1) / JOIN_RUNS), l.slices), dim3(256), 0, s, in.pair, n, w.run, w.runs, rows, width,
+        hipLaunchKernelGGL((join_runs_kernel<T, WHOLE>), dim3((unsigned)((w.runs + join_runs(l.lanes) - 1) / join_runs(l.lanes)), l.slices), dim3(256), 0, s, in.pair, n, w.run, w.runs, rows, width,
                            scale, (T *)dtable, ld_dtable, w.part, w.part_width, l.lanes);
         return last_launch();
     });
