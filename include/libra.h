@@ -380,10 +380,10 @@ int libra_embedding(const void *table, int64_t rows, int32_t width, int64_t ld_t
  * libra_embedding_backward - dtable[v,:] = scale * sum over all i with index[i] = v of dout[i,:]: the ids are sorted, the rows of an id
  * are added in fp32, the sum is rounded once to `dtype`.  The order of additions depends on the ids and n alone, so equal calls give
  * equal bits.  Rows that no id names become zeros; ids outside [0, rows) count for nothing.
- *   dout       device, n x width with row stride ld_dout;  index as in libra_embedding;  n < 2^31
+ *   dout       device, n x width with row stride ld_dout, width <= 2^21;  index as in libra_embedding;  n < 2^31
  *   dtable     device, rows x width with row stride ld_dtable, rows < 2^31 - 1; fully overwritten; none of the inputs
  *   workspace  device, 256-byte aligned, libra_embedding_backward_workspace() bytes, not needed after the call has run (n = 0: may be NULL)
- * Errors: as libra_embedding, and TOO_LARGE; BUFFER also for the workspace.
+ * Errors: as libra_embedding, and TOO_LARGE, UNSUPPORTED (width); BUFFER also for the workspace.
  */
 int libra_embedding_backward_workspace(int64_t n, int64_t rows, int32_t width, size_t *bytes);
 int libra_embedding_backward(const void *dout, int64_t ld_dout, int dtype, const void *index, int index_type, int64_t n, int64_t rows,

@@ -121,11 +121,12 @@ def test_gradient(dtype, kind, n, rows, width):
     assert torch.equal(got, lb.embedding_backward(dout, ids, rows, scale=SCALE))       # the same bits every time
 
 
-@pytest.mark.parametrize("n,rows", [(1 << 20, 1 << 20), (300007, 70000), (200000, 16), (1500001, (1 << 24) + 3)])
-def test_gradient_of_many_ids(n, rows):
+@pytest.mark.parametrize("n,rows,width", [(1 << 20, 1 << 20, 16), (300007, 70000, 16), (200000, 16, 16), (1500001, (1 << 24) + 3, 16), (100003, 2049 * 1024, 8), (50001, 2047, 40),
+                                          (50001, 2048, 1040), (40000, (1 << 21) - 1, 5), (16385, 3, 600), (20000, 1, 1)])
+def test_gradient_of_many_ids(n, rows, width):
     g = torch.Generator(device="cuda").manual_seed(1)
-    for kind in ("hot", "one"):
-        dout = torch.randn(n, 16, generator=g, device="cuda").bfloat16()
+    for kind in ("hot", "one", "ends", "uniform"):
+        dout = torch.randn(n, width, generator=g, device="cuda").bfloat16()
         ids = ids_of(n, rows, kind)
         got = lb.embedding_backward(dout, ids, rows, scale=SCALE)
         check_gradient(got, dout, ids, rows)

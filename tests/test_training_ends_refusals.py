@@ -62,7 +62,7 @@ def test_embedding_refuses(want, kw):
 
 @pytest.mark.parametrize("want,kw", [
     ("SHAPE", dict(n=-1)), ("SHAPE", dict(rows=-1)), ("SHAPE", dict(width=0)), ("SHAPE", dict(ld_dout=7)), ("SHAPE", dict(ld_out=7)),
-    ("TOO_LARGE", dict(n=1 << 31)), ("TOO_LARGE", dict(rows=(1 << 31) - 1)), ("DTYPE", dict(dtype=-1)), ("OPTION", dict(index_type=-1)),
+    ("TOO_LARGE", dict(n=1 << 31)), ("TOO_LARGE", dict(rows=(1 << 31) - 1)), ("UNSUPPORTED", dict(width=(1 << 21) + 1, ld_dout=1 << 22, ld_out=1 << 22)), ("DTYPE", dict(dtype=-1)), ("OPTION", dict(index_type=-1)),
     ("NULL", dict(dout=None)), ("NULL", dict(index=None)), ("NULL", dict(out=None)), ("NULL", dict(n=100000, ws=None)),
     ("BUFFER", dict(n=100000, ws=AT + 128)), ("BUFFER", dict(n=100000, ws_bytes=8)), ("BUFFER", dict(dout=AT + 1)), ("BUFFER", dict(index=AT + 4)), ("BUFFER", dict(out=AT + 1)),
 ])
