@@ -412,7 +412,7 @@ int libra_log_probs(const void *logits, int64_t n, int64_t classes, int64_t ld, 
 /*
  * libra_log_probs_backward - gradient of libra_log_probs with respect to the logits, rounded once to their type:
  * dlogits_j = scale * ([j = target] d + sum_a [j = top_index_a] d_a - p_j * (d + sum_a d_a + e * (log p_j + entropy))).
- *   entropy, stats, top_index  what the forward call wrote for the same logits, targets, top and scale
+ *   entropy, stats, top_index  what the forward call wrote for the same logits, targets, top and scale (the alternatives of a row differ)
  *   d_target, d_entropy, d_top  device, fp32[n], fp32[n], fp32[n * top]: d, e and d_a above; each may be NULL (zeros)
  *   dlogits    device, n x classes with row stride ld_dlogits, values of `dtype`; fully overwritten; none of the inputs
  * Errors: as libra_log_probs.

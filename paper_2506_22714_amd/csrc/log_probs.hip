@@ -16,7 +16,7 @@ using namespace libra;
 namespace {
 
 constexpr float INF = __builtin_inff(), LOWEST = -0x1.fffffep127f, LOG2E = 1.44269504088896340736f;
-constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 1024, MAX_PARTS = 64;
+constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 4096 - 7, MAX_PARTS = 64;
 static_assert(MAX_TOP <= WAVE_LANES, "a list of the best logits has a lane for each");
 
 // NaN if one of them is
@@ -111,70 +111,94 @@ __device__ inline void write_alternative(const Forward &f, int64_t i, int a, uin
     f.top_index[i * f.top + a] = class_of(key);
 }
 
-// ---- short rows: L lanes hold a row in registers, E logits each, in 16-byte pieces where every row is aligned to them ----
+// ---- short rows: L lanes hold a row in registers, E numbers each ----
+// They load the 16-byte pieces of memory that the row touches; a piece at an end of the row holds numbers of its neighbours, which count for
+// nothing.  (A load for every number where rows are not aligned: 65,536 x 500 bf16 46 us, not 22.)
+template <class T> struct Span {        // of all rows, and its whole pieces
+    const T *low, *high;
+    const T *first, *last;              // last < first: there is none
+    __device__ Span(const T *p, int64_t n, int64_t classes, int64_t ld) {
+        low = p;
+        high = p + (n - 1) * ld + classes;
+        first = reinterpret_cast<const T *>(((uintptr_t)low + 15) & ~(uintptr_t)15);
+        last = reinterpret_cast<const T *>((uintptr_t)high & ~(uintptr_t)15) - VECTOR<T>;
+    }
+};
+
 template <class T, int L, int E> struct ShortRow {
     static constexpr int W = VECTOR<T>, PIECES = E / W;
     float x[E];
-    __device__ static int class_at(int lane, int e) { return (lane + L * (e / W)) * W + e % W; }
-    __device__ void load(const T *row, int classes, int lane, bool whole, bool there) {
+    int before;                         // numbers in the first piece that are not the row's
+    __device__ int class_at(int lane, int e) const { return (lane + L * (e / W)) * W + e % W - before; }
+    __device__ void load(const Span<T> &span, const T *row, int classes, int lane) {
+        before = (int)((uintptr_t)row % 16 / sizeof(T));
+        const int end = (before + classes - 1) / W * W - before;        // the row's last piece: also for lanes beyond it
+        const T *at[PIECES];
+        uint4 raw[PIECES];
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int j = class_at(lane, p * W);
-            if (whole && there && j + W <= classes) unpack<T>(*reinterpret_cast<const uint4 *>(row + j), x + p * W);
-            else {
+            at[p] = row + min(class_at(lane, p * W), end);
+            const T *a = at[p] < span.first ? span.first : at[p] > span.last ? span.last : at[p];
+            if (span.first <= span.last) raw[p] = *reinterpret_cast<const uint4 *>(a);
+        }
 #pragma unroll
-                for (int k = 0; k < W; ++k) x[p * W + k] = there && j + k < classes ? load_as_float(row[j + k]) : -INF;
+        for (int p = 0; p < PIECES; ++p) {
+            unpack<T>(raw[p], x + p * W);
+            const int j = class_at(lane, p * W);
+            if ((at[p] < span.first || at[p] > span.last) && j + W > 0 && j < classes) {       // the ends of the first and the last row
+#pragma unroll
+                for (int k = 0; k < W; ++k) x[p * W + k] = j + k >= 0 && j + k < classes ? load_as_float(row[j + k]) : -INF;
             }
+#pragma unroll
+            for (int k = 0; k < W; ++k)
+                if (j + k < 0 || j + k >= classes) x[p * W + k] = -INF;
         }
     }
 };
 
+// What orders the logits of a short row, larger ones first and lower classes among equals: their 16 bits and the class, or 32 and the class
+template <class T> struct ShortKey {
+    typedef uint32_t type;
+    __device__ static uint32_t of(float x, int j) {
+        const T t = round_to<T>(x + 0.f);
+        const uint32_t u = __builtin_bit_cast(uint16_t, t);
+        return (x != x ? 0xffffu : u & 0x8000u ? ~u & 0xffffu : u | 0x8000u) << 16 | (0xffffu - (uint32_t)j);
+    }
+    __device__ static float logit(uint32_t key) {
+        const uint32_t r = key >> 16;
+        return load_as_float(__builtin_bit_cast(T, (uint16_t)(r == 0xffffu ? (uint32_t)__builtin_bit_cast(uint16_t, T(__builtin_nanf(""))) : r & 0x8000u ? r ^ 0x8000u : ~r)));
+    }
+    __device__ static int64_t class_at(uint32_t key) { return 0xffffu - (key & 0xffffu); }
+};
+template <> struct ShortKey<float> {
+    typedef uint64_t type;
+    __device__ static uint64_t of(float x, int j) { return key_of(x, (uint32_t)j); }
+    __device__ static float logit(uint64_t key) { return logit_of((uint32_t)(key >> 32)); }
+    __device__ static int64_t class_at(uint64_t key) { return class_of(key); }
+};
+
 // The best logits one after another: the best of each lane's, then of the group's; the lane that has it drops it.
 template <class T, int L, int E> __device__ inline void short_alternatives(const Forward &f, const ShortRow<T, L, E> &row, int64_t i, int lane, bool there, const Finished &r) {
-    uint32_t rank[E];
+    typedef ShortKey<T> Key;
+    typename Key::type key[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) rank[e] = ShortRow<T, L, E>::class_at(lane, e) < f.classes ? rank_of(row.x[e]) : 0;
+    for (int e = 0; e < E; ++e) {
+        const int j = row.class_at(lane, e);
+        key[e] = j >= 0 && j < f.classes ? Key::of(row.x[e], j) : 0;
+    }
     for (int a = 0; a < f.top; ++a) {
-        uint32_t best = rank[0];
-        int at = 0;
+        typename Key::type best = key[0];
 #pragma unroll
-        for (int e = 1; e < E; ++e)
-            if (rank[e] > best) best = rank[e], at = e;     // classes ascend with e
-        const uint64_t mine = (uint64_t)best << 32 | (0xffffffffu - (uint32_t)ShortRow<T, L, E>::class_at(lane, at));
-        const uint64_t key = over_group<L>(mine, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-        if (mine == key) {
+        for (int e = 1; e < E; ++e) best = key[e] > best ? key[e] : best;
+        best = over_group<L>(best, [](auto p, auto q) { return p > q ? p : q; });
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (e == at) rank[e] = 0;
+        for (int e = 0; e < E; ++e) key[e] = key[e] == best ? 0 : key[e];
+        if (there && lane == a % L) {
+            f.top_out[i * f.top + a] = r.logp(Key::logit(best), f.scale);
+            f.top_index[i * f.top + a] = Key::class_at(best);
         }
-        if (there && lane == a % L) write_alternative(f, i, a, key, r);
     }
 }
-
-template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits, bool whole) {
-    const int lane = threadIdx.x % L;
-    const float c = f.scale * LOG2E;
-    constexpr int EACH = 256 / L;
-    for (int64_t base = (int64_t)blockIdx.x * EACH; base < f.n; base += (int64_t)gridDim.x * EACH) {
-        const int64_t i = base + threadIdx.x / L;
-        const bool there = i < f.n;
-        ShortRow<T, L, E> row;
-        row.load(logits + i * f.ld, (int)f.classes, lane, whole, there);
-        float most = row.x[0];
-#pragma unroll
-        for (int e = 1; e < E; ++e) most = larger(most, row.x[e]);
-        Sums a;
-        a.template add<E>(row.x, over_group<L>(most, larger), c);
-        auto add = [](float x, float y) { return x + y; };
-        a.s = over_group<L>(a.s, add);
-        a.t = over_group<L>(a.t, add);
-        const Finished r = finish(a);
-        if (there && lane == 0) write_row(f, logits + i * f.ld, i, a, r);
-        if (f.top) short_alternatives(f, row, i, lane, there, r);
-    }
-}
-
-// ---- long rows: a workgroup walks a row, or a part of it where there are few rows ----
 
 // The best logits that a wave has seen, in descending order, one in each of the first `top` lanes.
 struct Best {
@@ -239,6 +263,45 @@ template <class F> __device__ inline void merge_lists(const uint64_t *keys, int 
     }
 }
 
+template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits) {
+    const int lane = threadIdx.x % L;
+    const float c = f.scale * LOG2E;
+    const Span<T> span(logits, f.n, f.classes, f.ld);
+    constexpr int ROWS = 256 / L;
+    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < f.n; base += (int64_t)gridDim.x * ROWS) {
+        const bool there = base + threadIdx.x / L < f.n;
+        const int64_t i = there ? base + threadIdx.x / L : f.n - 1;
+        ShortRow<T, L, E> row;
+        row.load(span, logits + i * f.ld, (int)f.classes, lane);
+        float mine = row.x[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) mine = larger(mine, row.x[e]);
+        Sums a;
+        a.template add<E>(row.x, over_group<L>(mine, larger), c);
+        auto add = [](float x, float y) { return x + y; };
+        a.s = over_group<L>(a.s, add);
+        a.t = over_group<L>(a.t, add);
+        const Finished r = finish(a);
+        if (there && lane == 0) write_row(f, logits + i * f.ld, i, a, r);
+        if constexpr (L < WAVE_LANES) {
+            if (f.top) short_alternatives(f, row, i, lane, there, r);
+        } else if (f.top) {
+            // `top` lanes have a maximum that reaches this rank: no logit below it is among the alternatives, and few others reach it.
+            // (One after another, as for shorter rows: 65,536 x 1,000 bf16 with 20 251 us, not 117.)
+            const float limit = logit_of(wave_kth(rank_of(mine), f.top));
+            Best best;
+#pragma unroll
+            for (int e = E - 1; e >= 0; --e) {
+                const int j = row.class_at(lane, e);
+                const bool near = !(row.x[e] < limit) && j >= 0 && j < f.classes;
+                if (__ballot(near)) best.insert(near ? key_of(row.x[e], (uint32_t)j) : 0, f.top);
+            }
+            if (there && lane < f.top) write_alternative(f, i, lane, best.key, r);
+        }
+    }
+}
+
+// ---- long rows: a workgroup walks a row, or a part of it where there are few rows ----
 struct Parts {                      // of rows that several workgroups share
     int32_t count;
     float *sums;                    // 3 for each part of each row
@@ -441,44 +504,52 @@ struct RowGradient {
     }
 };
 
-template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_backward_kernel(Backward g, const T *logits, T *out, bool whole) {
+// The alternatives' classes are written a second time, whole, by a lane each.  (In the registers that hold them: 65,536 x 1,000 bf16 with 20
+// alternatives 186 us, not 70.)
+template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_backward_kernel(Backward g, const T *logits, T *out) {
     typedef ShortRow<T, L, E> Row;
     const int lane = threadIdx.x % L;
-    constexpr int EACH = 256 / L;
-    for (int64_t base = (int64_t)blockIdx.x * EACH; base < g.n; base += (int64_t)gridDim.x * EACH) {
-        const int64_t i = min(base + threadIdx.x / L, g.n - 1);         // (rows behind the last one: the last one once more)
+    const Span<T> span(logits, g.n, g.classes, g.ld);
+    constexpr int ROWS = 256 / L;
+    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < g.n; base += (int64_t)gridDim.x * ROWS) {
+        const bool there = base + threadIdx.x / L < g.n;
+        const int64_t i = there ? base + threadIdx.x / L : g.n - 1;
+        const T *x = logits + i * g.ld;
+        T *o = out + i * g.ld_out;
         Row row;
-        row.load(logits + i * g.ld, (int)g.classes, lane, whole, true);
+        row.load(span, x, (int)g.classes, lane);
         RowGradient r;
         r.template load<L>(g, i, lane);
-        T *o = out + i * g.ld_out;
+        const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             row.x[e] = r.at(row.x[e], g.scale);
-            if (Row::class_at(lane, e) == r.target && !r.empty) row.x[e] = fmaf(g.scale, r.d, row.x[e]);
+            if (row.class_at(lane, e) == r.target && !r.empty) row.x[e] = fmaf(g.scale, r.d, row.x[e]);
         }
-        if (g.d_top && !r.empty)
-            for (int k = 0; k < g.top; ++k) {
-                const int64_t j = g.top_index[i * g.top + k];
-                const float more = g.scale * g.d_top[i * g.top + k];
+        if (there) {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (Row::class_at(lane, e) == j) row.x[e] += more;
+            for (int p = 0; p < Row::PIECES; ++p) {
+                const int j = row.class_at(lane, p * Row::W);
+                if (alike && j >= 0 && j + Row::W <= g.classes) *reinterpret_cast<uint4 *>(o + j) = pack<T>(row.x + p * Row::W);
+                else {
+#pragma unroll
+                    for (int k = 0; k < Row::W; ++k)
+                        if (j + k >= 0 && j + k < g.classes) o[j + k] = round_to<T>(row.x[p * Row::W + k]);
+                }
             }
-#pragma unroll
-        for (int p = 0; p < Row::PIECES; ++p) {
-            const int j = Row::class_at(lane, p * Row::W);
-            if (whole && j + Row::W <= g.classes) *reinterpret_cast<uint4 *>(o + j) = pack<T>(row.x + p * Row::W);
-            else {
-#pragma unroll
-                for (int k = 0; k < Row::W; ++k)
-                    if (j + k < g.classes) o[j + k] = round_to<T>(row.x[p * Row::W + k]);
+        }
+        if (g.d_top) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // behind what this wave has written
+            for (int k = lane; k < g.top; k += L) {
+                const int64_t j = g.top_index[i * g.top + k];
+                if (there && !r.empty && j >= 0 && j < g.classes)
+                    o[j] = round_to<T>(fmaf(g.scale, g.d_top[i * g.top + k] + (j == r.target ? r.d : 0.f), r.at(load_as_float(x[j]), g.scale)));
             }
         }
     }
 }
 
-// A workgroup takes a run of pieces of a row; the few classes that get more than p_j (...) are written a second time, whole.  Rows are
+// A workgroup takes a run of pieces of a row; the classes that get more than p_j (...) are written a second time, whole.  Rows are
 // taken from the last to the first: the forward pass has just read the last ones.
 template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
     constexpr int W = VECTOR<T>, U = 32 / W;
@@ -524,25 +595,14 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_bac
         }
         if (r.empty || (r.target < 0 && !g.d_top)) continue;        // the same for the whole workgroup
         __syncthreads();
-        // The first wave writes the alternatives, the second one the target unless it is among them.  (An index that comes twice gets both.)
+        // the first wave writes the alternatives, the second one the target unless it is among them
         if (wave < 2) {
             const bool listed = g.d_top && lane < g.top;
             int64_t j = listed ? g.top_index[i * g.top + lane] : -1;
-            float more = listed ? g.d_top[i * g.top + lane] : 0.f;
-            if (wave == 0) {
-                const float mine = more;
-                if (g.d_top)
-                    for (int a = 1; a < g.top; ++a) {
-                        const int other = (lane + a) % g.top;
-                        const int64_t k = (int64_t)__shfl((long long)j, other);
-                        const float d = __shfl(mine, other);
-                        if (listed && k == j) more += d;
-                    }
-                if (listed && j == r.target) more += r.d;
-            } else {
+            float more = listed && wave == 0 ? g.d_top[i * g.top + lane] + (j == r.target ? r.d : 0.f) : r.d;
+            if (wave == 1) {
                 const bool among = __ballot(listed && j == r.target) != 0;
                 j = lane == 0 && !among ? r.target : -1;
-                more = r.d;
             }
             if (j >= 0 && j >= low && j < high && j < g.classes) o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
         }
@@ -566,16 +626,22 @@ int32_t part_count(int64_t n, int64_t classes) {
 
 size_t part_bytes(int64_t n, int32_t count, int32_t top) { return count == 1 ? 0 : ((size_t)n * count * 12 + 255) / 256 * 256 + (size_t)n * count * top * 8; }
 
-// f(lanes of a row, logits of a lane)
-template <class F> int for_short(int64_t classes, F &&f) {
-    typedef std::integral_constant<int, 8> E8;
-    typedef std::integral_constant<int, 16> E16;
-    if (classes <= 64) return f(std::integral_constant<int, 8>{}, E8{});
-    if (classes <= 128) return f(std::integral_constant<int, 16>{}, E8{});
-    if (classes <= 256) return f(std::integral_constant<int, 32>{}, E8{});
-    if (classes <= 512) return f(std::integral_constant<int, 64>{}, E8{});
-    return f(std::integral_constant<int, 64>{}, E16{});
+// f(lanes of a row, numbers of a lane) for rows that with their neighbours' numbers in the first piece have `numbers`
+template <class F> int for_short(int64_t numbers, F &&f) {
+#define LIBRA_SHORT(L, E) \
+    if (numbers <= L * E) return f(std::integral_constant<int, L>{}, std::integral_constant<int, E>{});
+    LIBRA_SHORT(1, 16)
+    LIBRA_SHORT(4, 8)
+    LIBRA_SHORT(8, 8)
+    LIBRA_SHORT(16, 8)
+    LIBRA_SHORT(32, 8)
+    LIBRA_SHORT(64, 8)
+    LIBRA_SHORT(64, 16)
+    LIBRA_SHORT(64, 32)
+#undef LIBRA_SHORT
+    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
 }
+template <class T> int64_t short_numbers(const T *x, int64_t classes, int64_t ld) { return classes + (aligned_to(x, 16) && ld % VECTOR<T> == 0 ? 0 : VECTOR<T> - 1); }
 
 constexpr int64_t MOST_WORKGROUPS = 1 << 23;        // the threads of a launch are counted in 32 bits
 
@@ -611,11 +677,10 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
     return for_dtype(dtype, [&](auto tag) {
         typedef decltype(tag) T;
         const T *x = (const T *)logits;
-        if (classes <= SHORT_CLASSES) return for_short(classes, [&](auto lanes, auto each) {
+        if (classes <= SHORT_CLASSES) return for_short(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
-            const bool whole = aligned_to(x, 16) && ld % VECTOR<T> == 0;
             const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
-            hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x, whole);
+            hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x);
             return last_launch();
         });
         hipLaunchKernelGGL((long_rows_kernel<T>), dim3((unsigned)std::min<int64_t>(n * parts.count, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
@@ -643,11 +708,10 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
         typedef decltype(tag) T;
         const T *x = (const T *)logits;
         T *o = (T *)dlogits;
-        if (classes <= SHORT_CLASSES) return for_short(classes, [&](auto lanes, auto each) {
+        if (classes <= SHORT_CLASSES) return for_short(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
-            const bool whole = aligned_to(x, 16) && ld % VECTOR<T> == 0 && aligned_to(o, 16) && ld_dlogits % VECTOR<T> == 0;
             const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
-            hipLaunchKernelGGL((short_rows_backward_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, g, x, o, whole);
+            hipLaunchKernelGGL((short_rows_backward_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, g, x, o);
             return last_launch();
         });
         const int64_t pieces = (classes + 2 * VECTOR<T> - 2) / VECTOR<T>, run = 32 / VECTOR<T> * LONG_THREADS, runs = (pieces + run - 1) / run;
