@@ -168,6 +168,7 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
         for (int32_t r = group; r < mine; r += groups)
             if (!named[r]) zero.store(dtable + (low + r) * ld_dtable + c);
     }
+    if (m == 0) return;                                         // the same for the whole workgroup
 
     // into the order of their rows (`start`: where a row's ids begin)
     {
@@ -246,10 +247,15 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
 #pragma unroll
         for (int w = 0; w < P::W; ++w) part[w * OWNER_THREADS + threadIdx.x] = sum.x[w];
         __syncthreads();
-        if (group == 0 && there) {
-            for (int g = 1; g < groups; ++g)
+        for (int half = groups / 2; half > 0; half /= 2) {       // the groups' sums in pairs
+            if (group < half)
 #pragma unroll
-                for (int w = 0; w < P::W; ++w) sum.x[w] += part[w * OWNER_THREADS + g * lanes + threadIdx.x];
+                for (int w = 0; w < P::W; ++w) part[w * OWNER_THREADS + threadIdx.x] += part[w * OWNER_THREADS + half * lanes + threadIdx.x];
+            __syncthreads();
+        }
+        if (group == 0 && there) {
+#pragma unroll
+            for (int w = 0; w < P::W; ++w) sum.x[w] = part[w * OWNER_THREADS + threadIdx.x];
             sum.scale(scale);
             sum.store(dtable + (low + r) * ld_dtable + c);
         }
@@ -568,10 +574,15 @@ __global__ __launch_bounds__(256) void join_runs_kernel(const uint2 *pair, int64
 #pragma unroll
         for (int w = 0; w < P::W; ++w) shared[w * 256 + threadIdx.x] = sum.x[w];
         __syncthreads();
-        if (group == 0 && there) {
-            for (int g = 1; g < groups; ++g)
+        for (int half = groups / 2; half > 0; half /= 2) {
+            if (group < half)
 #pragma unroll
-                for (int w = 0; w < P::W; ++w) sum.x[w] += shared[w * 256 + g * lanes + threadIdx.x];
+                for (int w = 0; w < P::W; ++w) shared[w * 256 + threadIdx.x] += shared[w * 256 + half * lanes + threadIdx.x];
+            __syncthreads();
+        }
+        if (group == 0 && there) {
+#pragma unroll
+            for (int w = 0; w < P::W; ++w) sum.x[w] = shared[w * 256 + threadIdx.x];
             sum.scale(scale);
             sum.store(dtable + row * ld_dtable + c);
         }
