@@ -17,6 +17,7 @@ using namespace libra;
 namespace {
 
 constexpr int STATE_BLOCK = LIBRA_ADAMW_BLOCK, LAUNCH_TENSORS = 32;
+static_assert(LAUNCH_TENSORS % 4 == 0, "searched by fours");
 constexpr int64_t LAUNCH_BLOCKS = 1 << 22;      // the threads of a launch are counted in 32 bits
 
 struct Tensors {                    // of one launch, in its arguments: nothing is copied to the device beforehand
@@ -149,9 +150,11 @@ constexpr int EACH = 8, GROUP_BLOCKS = 256 * EACH / STATE_BLOCK, BLOCK_LANES = S
 template <class T, bool BITS8>
 __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
     read_step(s);
+    // the last tensor that begins at this workgroup or before: four at a time (all 32: 14 us of scalar instructions for 67 M elements)
     int k = -1;
+    for (int j = 0; j < LAUNCH_TENSORS && list.first[j] <= (int)blockIdx.x; j += 4)
 #pragma unroll
-    for (int j = 0; j < LAUNCH_TENSORS; ++j) k += list.first[j] <= (int)blockIdx.x;     // (all loaded at once; behind the last tensor: none)
+        for (int u = 0; u < 4; ++u) k += list.first[j + u] <= (int)blockIdx.x;
     const libra_adamw_tensor_t &t = list.t[k];
     const int64_t i = (list.begin[k] + (blockIdx.x - list.first[k])) * (GROUP_BLOCKS * STATE_BLOCK) + threadIdx.x * EACH, n = t.n;
     const bool whole = list.aligned[k] && i + EACH <= n;
