@@ -103,21 +103,21 @@ template <class C> __device__ inline int32_t rank_in_wave(uint32_t digit, int bi
 
 // -- few ids --
 constexpr int OWNER_THREADS = 1024, OWNER_WAVES = OWNER_THREADS / WAVE_LANES, OWNER_PLACE_BITS = 14, OWNER_MAX_IDS = 1 << OWNER_PLACE_BITS;
-constexpr int OWNER_ROW_BITS = 9, OWNER_ROWS = 1 << OWNER_ROW_BITS, OWNER_LONG = 32;    // rows with more ids than that are added up by the whole workgroup
+constexpr int OWNER_ROW_BITS = 10, OWNER_ROWS = 1 << OWNER_ROW_BITS, OWNER_LONG = 32;    // rows with more ids than that are added up by the whole workgroup
 
 template <class T, bool WHOLE, int MOST>
 __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int64_t ld_dout, const void *index, int index_type, int32_t n, int64_t rows, int32_t width,
-                                                              int32_t owned, float scale, T *dtable, int64_t ld_dtable, int lanes) {
+                                                              int32_t owned, int row_bits, float scale, T *dtable, int64_t ld_dtable, int lanes) {
     typedef Piece<T, WHOLE> P;
     constexpr int IDS = MOST / OWNER_THREADS;
     __shared__ uint32_t list[MOST];                             // row in this run << OWNER_PLACE_BITS | place, n at most
     __shared__ int32_t start[OWNER_ROWS], total[OWNER_WAVES], long_rows[OWNER_MAX_IDS / OWNER_LONG], longs;
     __shared__ uint8_t named[OWNER_ROWS];                       // the row has ids
     __shared__ union {                                          // first the one, then the other
-        int32_t count[OWNER_WAVES][OWNER_ROWS];
+        uint16_t count[OWNER_WAVES][OWNER_ROWS];
         float part[OWNER_THREADS * 8];
     } shared;
-    int32_t(&count)[OWNER_WAVES][OWNER_ROWS] = shared.count;
+    uint16_t(&count)[OWNER_WAVES][OWNER_ROWS] = shared.count;
     float(&part)[OWNER_THREADS * 8] = shared.part;
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
     const int64_t low = (int64_t)blockIdx.x * owned;
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
             to += __popcll(those);
         }
     }
-    for (int r = threadIdx.x; r < OWNER_WAVES * OWNER_ROWS; r += OWNER_THREADS) (&count[0][0])[r] = 0;
+    for (int r = threadIdx.x; r < OWNER_WAVES * OWNER_ROWS / 2; r += OWNER_THREADS) reinterpret_cast<uint32_t *>(count)[r] = 0;
     if (threadIdx.x == 0) longs = 0;
     __syncthreads();
     if (there) {                                                // the zeros, on their way while the list is sorted
@@ -180,18 +180,23 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
             if (b < each) {
                 const int32_t q = (wave * each + b) * WAVE_LANES + lane;
                 item[b] = q < m ? list[q] : 0;
-                rank[b] = rank_in_wave(item[b] >> OWNER_PLACE_BITS, OWNER_ROW_BITS, q < m, count[wave]);
+                rank[b] = rank_in_wave(item[b] >> OWNER_PLACE_BITS, row_bits, q < m, count[wave]);
             }
         }
         __syncthreads();
-        // a row's number over all waves, then the sum of the rows before: OWNER_ROWS threads
+        // a row's number over all waves, then the sum of the rows before
+        static_assert(OWNER_ROWS == OWNER_THREADS, "a thread for each row");
         int32_t sum = 0;
-        if (threadIdx.x < OWNER_ROWS)
+        {
+            uint16_t in[OWNER_WAVES];
+#pragma unroll
+            for (int w = 0; w < OWNER_WAVES; ++w) in[w] = count[w][threadIdx.x];
+#pragma unroll
             for (int w = 0; w < OWNER_WAVES; ++w) {
-                const int32_t c = count[w][threadIdx.x];
-                count[w][threadIdx.x] = sum;
-                sum += c;
+                count[w][threadIdx.x] = (uint16_t)sum;
+                sum += in[w];
             }
+        }
         int32_t up_to = sum;
         for (int d = 1; d < WAVE_LANES; d *= 2) {
             const int32_t y = __shfl_up(up_to, d);
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(OWNER_THREADS) void owner_kernel(const T *dout, int
         if (lane == WAVE_LANES - 1) total[wave] = up_to;
         __syncthreads();
         for (int w = 0; w < wave; ++w) up_to += total[w];
-        if (threadIdx.x < OWNER_ROWS) start[threadIdx.x] = up_to - sum;
+        start[threadIdx.x] = up_to - sum;
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < IDS; ++b) {
@@ -601,8 +606,12 @@ Layout layout(int32_t width, int piece) {
     return {lanes, (unsigned)((pieces + lanes - 1) / lanes)};
 }
 
-// Two workgroups for every compute unit, as long as their rows can be told apart in one pass.
-int64_t owned_rows(int64_t rows) { return std::min<int64_t>(std::max<int64_t>((rows + 511) / 512, 1), OWNER_ROWS); }
+// As many workgroups as the compute units hold at once, as long as their rows can be told apart in one pass: two for each, one where a
+// workgroup has LDS for more than half of the most ids.
+int64_t owned_rows(int64_t n, int64_t rows) {
+    const int64_t owners = n <= OWNER_MAX_IDS / 2 ? 512 : 256;
+    return std::min<int64_t>(std::max<int64_t>((rows + owners - 1) / owners, 1), OWNER_ROWS);
+}
 // Every owner reads all ids: they come out of the L2s, at some 10 TB/s, so 2^24 of them cost about as much as the launches of the sort.
 bool few_ids(int64_t n, int64_t rows) { return n <= OWNER_MAX_IDS && n * ((rows + OWNER_ROWS - 1) / OWNER_ROWS) <= 1 << 24; }
 
@@ -700,13 +709,14 @@ extern "C" int libra_embedding_backward(const void *dout, int64_t ld_dout, int d
         typedef decltype(tag) T;
         constexpr bool WHOLE = decltype(whole)::value;
         const Layout l = layout(width, Piece<T, WHOLE>::W);
-        const int64_t owned = owned_rows(rows);
+        const int64_t owned = owned_rows(n, rows);
+        int row_bits = 1;
+        while (1 << row_bits < owned) ++row_bits;
         const dim3 grid((unsigned)((rows + owned - 1) / owned), l.slices);
         auto launch = [&](auto most) {
             hipLaunchKernelGGL((owner_kernel<T, WHOLE, decltype(most)::value>), grid, dim3(OWNER_THREADS), 0, s, (const T *)dout, ld_dout, index, index_type, (int32_t)n, rows, width,
-                               (int32_t)owned, scale, (T *)dtable, ld_dtable, l.lanes);
+                               (int32_t)owned, row_bits, scale, (T *)dtable, ld_dtable, l.lanes);
         };
-        // two workgroups on a compute unit with half a list, one with a whole one
         if (n <= OWNER_MAX_IDS / 2) launch(std::integral_constant<int, OWNER_MAX_IDS / 2>{});
         else launch(std::integral_constant<int, OWNER_MAX_IDS>{});
         return last_launch();
