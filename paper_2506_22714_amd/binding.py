@@ -797,12 +797,12 @@ class Plan:
 # ---- the ends of a training step: no plan, any GPU (the call is made on the device and the current stream of its operands) ----
 def _launch(call, what: str, like, *args):
     """call(*args, stream) on the device of the tensor `like`."""
-    torch = _torch
-    if like.get_device() == torch.cuda.current_device():
+    cuda = _torch.cuda
+    if like.get_device() == cuda.current_device():
         rc = call(*args, _stream())
     else:
-        with torch.cuda.device(like.device):
-            rc = call(*args, torch.cuda.current_stream().cuda_stream)
+        with cuda.device(like.device):
+            rc = call(*args, cuda.current_stream().cuda_stream)
     if rc:
         _check(rc, what)
 
@@ -842,16 +842,16 @@ def _index_code(t, name: str, like) -> int:
     torch = _torch
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous int32 or int64 torch tensor")
-    if not t.is_cuda or t.get_device() != like.get_device():
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name}: must be a tensor on {like.device}")
     return INDEX_I64 if t.dtype is torch.int64 else INDEX_I32
 
 
 def _fp32_on(t, name: str, shape, like):
     torch = _torch
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous float32 torch tensor of shape {tuple(shape)}")
-    if not t.is_cuda or t.get_device() != like.get_device():
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name}: must be a tensor on {like.device}")
     return t.data_ptr()
 
@@ -866,7 +866,7 @@ def embedding(table, index, scale: float = 1.0, out=None):
     if width < 1:
         raise ValueError("table: rows of no elements")
     if out is None:
-        out, ld_out = torch.empty((*index.shape, width), dtype=table.dtype, device=table.device), width
+        out, ld_out = torch.empty(*index.shape, width, dtype=table.dtype, device=table.device), width
     else:
         _rows_of(out, "out", width, like=table)
         if out.shape[0] != n:
@@ -889,7 +889,7 @@ def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
     if index.numel() != n:
         raise ValueError(f"index: {index.numel()} ids for {n} rows of dout")
     if out is None:
-        out = torch.empty((rows, width), dtype=dout.dtype, device=dout.device)
+        out = torch.empty(rows, width, dtype=dout.dtype, device=dout.device)
     else:
         _rows_of(out, "out", width, like=dout)
         if out.shape[0] != rows:
@@ -925,9 +925,9 @@ def log_probs(logits, targets=None, top: int = 0, scale: float = 1.0) -> LogProb
     device = logits.device
     target = torch.empty(n, dtype=torch.float32, device=device) if targets is not None else None
     entropy = torch.empty(n, dtype=torch.float32, device=device)
-    stats = torch.empty((n, 2), dtype=torch.float32, device=device)
-    best = torch.empty((n, top), dtype=torch.float32, device=device)
-    index = torch.empty((n, top), dtype=torch.int64, device=device)
+    stats = torch.empty(n, 2, dtype=torch.float32, device=device)
+    best = torch.empty(n, top, dtype=torch.float32, device=device)
+    index = torch.empty(n, top, dtype=torch.int64, device=device)
     ws = torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
     _launch(lib().libra_log_probs, "libra_log_probs", logits, logits.data_ptr(), n, classes, _ld(logits), dtype,
             targets.data_ptr() if targets is not None else 0, kind, top, scale, target.data_ptr() if targets is not None else 0,
@@ -955,7 +955,7 @@ def log_probs_backward(logits, result: LogProbs, targets=None, d_target=None, d_
     grads = [0 if t is None else _fp32_on(t, name, want, logits)
              for t, name, want in ((d_target, "d_target", (n,)), (d_entropy, "d_entropy", (n,)), (d_top, "d_top", (n, top)))]
     if out is None:
-        out = torch.empty((n, classes), dtype=logits.dtype, device=logits.device)
+        out = torch.empty(n, classes, dtype=logits.dtype, device=logits.device)
     else:
         _rows_of(out, "out", classes, like=logits)
         if out.shape[0] != n:

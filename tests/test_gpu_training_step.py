@@ -144,6 +144,18 @@ def test_a_whole_step_replayed_from_a_graph():
     sm.close()
 
 
+def test_log_probs_without_targets():
+    from paper_2506_22714_amd import autograd as ag
+    x = torch.randn(5, 9, device="cuda", requires_grad=True)
+    logp, h, top, classes = ag.log_probs(x, top=2, scale=1.5)
+    assert logp is None
+    (h.sum() - top[:, 1].sum()).backward()
+    z = x.detach().double().requires_grad_()
+    lp = torch.log_softmax(1.5 * z, 1)
+    (-(lp.exp() * lp).sum() - lp.gather(1, classes[:, 1:]).sum()).backward()
+    assert float((x.grad.double() - z.grad).abs().max()) < 2.0 ** -24 * 400
+
+
 def test_no_second_derivatives():
     from paper_2506_22714_amd import autograd as ag
     w = torch.randn(5, 4, device="cuda", requires_grad=True)
