@@ -397,9 +397,12 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
             }
             __builtin_amdgcn_wave_barrier();
             for (int q = 0; q < many; q += WAVE_LANES) {
-                const bool there = q + lane < many;
-                const int at = there ? reaching[wave][q + lane] : 0;
+                const int at = reaching[wave][min(q + lane, many - 1)];
                 const int64_t v = super + (at / WAVE_LANES) * ROUND + wave * WAVE_LANES + at % WAVE_LANES;
+                // the best that these logits can be: their maximum, of the lowest class (rows of equal logits, masked ones among them, have little to read)
+                const uint32_t lowest = (uint32_t)max(v * W - before, (int64_t)0);
+                const bool there = q + lane < many && ((uint64_t)rank_of(maxima[at / WAVE_LANES][wave * WAVE_LANES + at % WAVE_LANES]) << 32 | (0xffffffffu - lowest)) > best.limit;
+                if (!__ballot(there)) continue;
                 uint4 again[U];
                 float y[N];
 #pragma unroll
