@@ -423,7 +423,7 @@ int libra_log_probs_backward(const void *logits, int64_t n, int64_t classes, int
                              void *stream);
 
 /*
- * libra_adamw - one AdamW step over `count` tensors, in one launch for up to 32 tensors of a type:
+ * libra_adamw - one AdamW step over `count` tensors, one launch for up to 32 tensors of a type:
  *   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g g,   p <- (1 - lr wd) p - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
  * in fp32; a 16-bit parameter is rounded once, from p or from its copy in 32 bits where it has one (`master`, the number that is kept).
  * state_bits = 32: m and v in fp32.  state_bits = 8: m and sqrt(v) as OCP e4m3 numbers, times a power of two (fp32, in first_scales and

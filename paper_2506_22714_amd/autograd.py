@@ -14,6 +14,9 @@ and at the ends of a training step, before and behind the sparse layers:
                      dW_v = scale sum_{index_i = v} dout_i
   log p = log softmax(scale x), H = -sum p log p
                      dx_j = scale ([j = target] d + sum_a [j = top_a] d_a - p_j (d + sum_a d_a + e (log p_j + H)))
+
+A backward pass may be captured into a HIP graph.  Let no graph of an eager pass over the same parameters live on then: torch's nodes that
+add up their gradients belong to that pass's stream, and the capture ends with an error or takes the process with it.
 """
 from __future__ import annotations
 

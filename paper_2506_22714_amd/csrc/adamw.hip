@@ -7,6 +7,9 @@
 // 0.1 % a step, and e4m3 numbers are 6 to 12 % apart.  The chances are a hash of (seed, step, tensor, element), so a step gives the same
 // result every time.  A root above zero never becomes zero: it divides.  The new parameter is made from the states before they are rounded.
 // No product is contracted with a sum: what is rounded to 8 bits is then the same on every machine with IEEE arithmetic.
+//
+// Bound by memory: 16.8 M fp32 elements with 32-bit states 90 us, 67 M bf16 with copies in 32 bits and 8-bit states 210 us (5.2 TB/s).
+// Without the copies 8-bit states are bound by the vector ALUs: 176 us, 3.8 TB/s.
 #include <algorithm>
 #include <cmath>
 

@@ -35,7 +35,8 @@ template <class T, bool WHOLE> struct Piece {
     }
 };
 
-// ---- lookup: LOOKUP_ROWS rows of each group of lanes in flight ----
+// ---- lookup ----
+// Four rows of each group of lanes in flight: 1,000,003 rows of 128 bytes in 39 us, 5 TB/s (one row of a wave at a time: 137 us).
 constexpr int LOOKUP_ROWS = 4;
 
 template <class T, bool WHOLE>
@@ -102,6 +103,8 @@ template <class C> __device__ inline int32_t rank_in_wave(uint32_t digit, int bi
 }
 
 // -- few ids --
+// 8,191 ids on 2^17 rows of 256 bytes: 17 us, of which the zeros are 6.4 at the rate of memory; the rest is latency, the same for all
+// workgroups, which run at once: ids from the L2s, LDS sort, rows of dout.  Loads are issued together, outside branches (24 us before).
 constexpr int OWNER_THREADS = 1024, OWNER_WAVES = OWNER_THREADS / WAVE_LANES, OWNER_PLACE_BITS = 14, OWNER_MAX_IDS = 1 << OWNER_PLACE_BITS;
 constexpr int OWNER_ROW_BITS = 10, OWNER_ROWS = 1 << OWNER_ROW_BITS, OWNER_LONG = 32;    // rows with more ids than that are added up by the whole workgroup
 
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int6
     }
 }
 
-// Runs of `run` pairs, a group of lanes each.  The row that a run begins in the middle of, and the one that goes on behind it, leave their
+// Runs of `run` pairs, a group of lanes each, eight rows of dout in flight: 41 us for 2^20 rows of 128 bytes, 5 TB/s with what is written.  The row that a run begins in the middle of, and the one that goes on behind it, leave their
 // sums in `part` (two rows of fp32 for each run); a row that fills the whole run and goes on at both ends leaves the first of them.
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld_dout, const uint2 *pair, int64_t n, int32_t run, int64_t rows, int32_t width, float scale,
