@@ -30,6 +30,9 @@ template <class T> __device__ inline uint4 pack(const float *f) {
     return v;
 }
 
+// 16 bytes that begin at any element: one load or store too (memory accesses need no alignment here)
+struct __attribute__((packed, aligned(2))) Unaligned { uint32_t x[4]; };
+
 // What the lane `STEP` further (by exclusive or of lane numbers, once the steps below it have been taken) holds: moves inside a row of
 // 16 lanes, shuffles beyond.
 template <int STEP> __device__ inline uint32_t lane_across(uint32_t x) {

@@ -525,7 +525,6 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
         row.load(span, x, (int)g.classes, lane);
         RowGradient r;
         r.template load<L>(g, i, lane);
-        const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             row.x[e] = r.at(row.x[e], g.scale);
@@ -535,7 +534,7 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
 #pragma unroll
             for (int p = 0; p < Row::PIECES; ++p) {
                 const int j = row.class_at(lane, p * Row::W);
-                if (alike && j >= 0 && j + Row::W <= g.classes) *reinterpret_cast<uint4 *>(o + j) = pack<T>(row.x + p * Row::W);
+                if (j >= 0 && j + Row::W <= g.classes) *reinterpret_cast<Unaligned *>(o + j) = __builtin_bit_cast(Unaligned, pack<T>(row.x + p * Row::W));
                 else {
 #pragma unroll
                     for (int k = 0; k < Row::W; ++k)
@@ -566,7 +565,7 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_bac
         const int before = (int)((uintptr_t)x % 16 / sizeof(T));
         const int64_t first = run * (U * LONG_THREADS), low = first * W - before, high = low + (int64_t)U * LONG_THREADS * W;
         RowGradient r;
-        if ((uintptr_t)o % 16 == (uintptr_t)x % 16 && low >= 0 && high <= g.classes) {
+        if (low >= 0 && high <= g.classes) {
             uint4 raw[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + low + (u * LONG_THREADS + threadIdx.x) * W);
@@ -577,20 +576,19 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_bac
                 unpack<T>(raw[u], y);
 #pragma unroll
                 for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
-                *reinterpret_cast<uint4 *>(o + low + (u * LONG_THREADS + threadIdx.x) * W) = pack<T>(y);
+                *reinterpret_cast<Unaligned *>(o + low + (u * LONG_THREADS + threadIdx.x) * W) = __builtin_bit_cast(Unaligned, pack<T>(y));
             }
-        } else {
-            const bool alike = (uintptr_t)o % 16 == (uintptr_t)x % 16;
+        } else {                                // the first and the last run of a row
             r.load<WAVE_LANES>(g, i, lane);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t j = low + (u * LONG_THREADS + threadIdx.x) * W;
                 float y[W];
-                if (alike && j >= 0 && j + W <= g.classes) {
+                if (j >= 0 && j + W <= g.classes) {
                     unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
 #pragma unroll
                     for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
-                    *reinterpret_cast<uint4 *>(o + j) = pack<T>(y);
+                    *reinterpret_cast<Unaligned *>(o + j) = __builtin_bit_cast(Unaligned, pack<T>(y));
                 } else {
 #pragma unroll
                     for (int k = 0; k < W; ++k)
