@@ -142,12 +142,18 @@ def edge_softmax(sm: SparseMatrix, scores: torch.Tensor, scale: float = 1.0) -> 
     return _EdgeSoftmax.apply(sm, scores, scale)
 
 
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    """x, copied if its rows are not contiguous (what lies between them may be anything)."""
+    x = x.detach()
+    return x if x.dim() != 2 or (x.stride(1) == 1 and x.stride(0) >= x.shape[1]) else x.contiguous()
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table: torch.Tensor, index: torch.Tensor, scale: float):
         ctx.rows, ctx.scale = table.shape[0], scale
         ctx.save_for_backward(index)
-        return lb.embedding(table.detach(), index, scale)
+        return lb.embedding(_rows(table), index, scale)
 
     @staticmethod
     @once_differentiable
@@ -159,7 +165,7 @@ class _Embedding(torch.autograd.Function):
 class _LogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits: torch.Tensor, targets, top: int, scale: float):
-        r = lb.log_probs(logits.detach(), targets, top, scale)
+        r = lb.log_probs(_rows(logits), targets, top, scale)
         ctx.scale = scale
         ctx.save_for_backward(logits, targets, r.entropy, r.top_index, r.stats)
         ctx.mark_non_differentiable(r.top_index)
@@ -171,7 +177,7 @@ class _LogProbs(torch.autograd.Function):
     def backward(ctx, d_target, d_entropy, d_top, _):
         logits, targets, entropy, top_index, stats = ctx.saved_tensors
         parts = [None if d is None else d.float().contiguous() for d in (d_target, d_entropy, d_top)]
-        return lb.log_probs_backward(logits.detach(), lb.LogProbs(None, entropy, None, top_index, stats), targets, *parts, scale=ctx.scale), None, None, None
+        return lb.log_probs_backward(_rows(logits), lb.LogProbs(None, entropy, None, top_index, stats), targets, *parts, scale=ctx.scale), None, None, None
 
 
 def embedding(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0) -> torch.Tensor:

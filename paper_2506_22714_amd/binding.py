@@ -888,13 +888,13 @@ def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
         raise ValueError("dout: rows of no elements")
     if index.numel() != n:
         raise ValueError(f"index: {index.numel()} ids for {n} rows of dout")
+    nb = libra_embedding_backward_workspace(n, rows, width)
     if out is None:
         out = torch.empty(rows, width, dtype=dout.dtype, device=dout.device)
     else:
         _rows_of(out, "out", width, like=dout)
         if out.shape[0] != rows:
             raise ValueError(f"out: {out.shape[0]} rows, expected {rows}")
-    nb = libra_embedding_backward_workspace(n, rows, width)
     ws = torch.empty(nb, dtype=torch.uint8, device=dout.device)
     _launch(lib().libra_embedding_backward, "libra_embedding_backward", dout, dout.data_ptr(), _ld(dout), dtype, index.data_ptr(), kind, n, rows,
             width, scale, out.data_ptr(), _ld(out), ws.data_ptr(), nb)

@@ -8,8 +8,9 @@
 // result every time.  A root above zero never becomes zero: it divides.  The new parameter is made from the states before they are rounded.
 // No product is contracted with a sum: what is rounded to 8 bits is then the same on every machine with IEEE arithmetic.
 //
-// Bound by memory: 16.8 M fp32 elements with 32-bit states 90 us, 67 M bf16 with copies in 32 bits and 8-bit states 210 us (5.2 TB/s).
-// Without the copies 8-bit states are bound by the vector ALUs: 176 us, 3.8 TB/s.
+// Bound by memory: 16.8 M fp32 elements with 32-bit states 90 us, 67 M bf16 with copies in 32 bits and 8-bit states 204 us (5.3 TB/s),
+// wherever the tensors begin (by single elements where they are not aligned: 484 us, not 218).  Without the copies 8-bit states are bound
+// by the vector ALUs: 167 us, 4.0 TB/s.
 #include <algorithm>
 #include <cmath>
 
@@ -27,7 +28,6 @@ struct Tensors {                    // of one launch, in its arguments: nothing 
     libra_adamw_tensor_t t[LAUNCH_TENSORS];
     int32_t first[LAUNCH_TENSORS];  // workgroup that each begins with
     int64_t begin[LAUNCH_TENSORS];  // and the workgroup of the tensor that this one is
-    bool aligned[LAUNCH_TENSORS];   // every array to 16 bytes
     int32_t count;
 };
 
@@ -105,28 +105,31 @@ __device__ inline Element updated(const Step &s, float p, float g, float m, floa
     return e;
 }
 
-// N neighbouring numbers from `i` on, in 16-byte pieces if `whole`; those from `n` on are zeros, and are not written
+// N neighbouring numbers from `i` on, in pieces of up to 16 bytes that begin anywhere if `whole`; those from `n` on are zeros, and are not written
 template <class T, int N> struct Run {
     T x[N];
+    static constexpr int PIECE = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16, PIECES = N * (int)sizeof(T) / PIECE;
+    struct __attribute__((packed, aligned(1))) Piece { uint32_t x[PIECE / 4]; };
     __device__ void load(const T *p, int64_t i, int64_t n, bool whole) {
-        constexpr int BYTES = N * (int)sizeof(T);
         if (whole) {
-            if constexpr (BYTES >= 16) {
 #pragma unroll
-                for (int k = 0; k < BYTES / 16; ++k) reinterpret_cast<uint4 *>(x)[k] = reinterpret_cast<const uint4 *>(p + i)[k];
-            } else *reinterpret_cast<uint2 *>(x) = *reinterpret_cast<const uint2 *>(p + i);
+            for (int k = 0; k < PIECES; ++k) {
+                const Piece q = reinterpret_cast<const Piece *>(p + i)[k];
+                __builtin_memcpy(x + k * (N / PIECES), &q, PIECE);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) x[k] = i + k < n ? p[i + k] : T(0);
         }
     }
     __device__ void store(T *p, int64_t i, int64_t n, bool whole) const {
-        constexpr int BYTES = N * (int)sizeof(T);
         if (whole) {
-            if constexpr (BYTES >= 16) {
 #pragma unroll
-                for (int k = 0; k < BYTES / 16; ++k) reinterpret_cast<uint4 *>(p + i)[k] = reinterpret_cast<const uint4 *>(x)[k];
-            } else *reinterpret_cast<uint2 *>(p + i) = *reinterpret_cast<const uint2 *>(x);
+            for (int k = 0; k < PIECES; ++k) {
+                Piece q;
+                __builtin_memcpy(&q, x + k * (N / PIECES), PIECE);
+                reinterpret_cast<Piece *>(p + i)[k] = q;
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k)
@@ -135,16 +138,22 @@ template <class T, int N> struct Run {
     }
 };
 
-// Codes of N elements
+// Codes of N elements, four in a word
 template <int N> __device__ inline void load_codes(Run<uint32_t, N / 4> &r, const uint8_t *p, int64_t i, int64_t n, bool whole) {
-    Run<uint8_t, N> bytes;
-    bytes.load(p, i, n, whole);
-    __builtin_memcpy(r.x, bytes.x, N);
+    if (whole) r.load(reinterpret_cast<const uint32_t *>(p + i), 0, 0, true);
+    else {
+        Run<uint8_t, N> bytes;
+        bytes.load(p, i, n, false);
+        __builtin_memcpy(r.x, bytes.x, N);
+    }
 }
 template <int N> __device__ inline void store_codes(const Run<uint32_t, N / 4> &r, uint8_t *p, int64_t i, int64_t n, bool whole) {
-    Run<uint8_t, N> bytes;
-    __builtin_memcpy(bytes.x, r.x, N);
-    bytes.store(p, i, n, whole);
+    if (whole) r.store(reinterpret_cast<uint32_t *>(p + i), 0, 0, true);
+    else {
+        Run<uint8_t, N> bytes;
+        __builtin_memcpy(bytes.x, r.x, N);
+        bytes.store(p, i, n, false);
+    }
 }
 
 // A workgroup takes eight blocks of 256 elements, a thread eight neighbouring elements: 32 lanes have a block of 8-bit states.
@@ -160,7 +169,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors list, Step s) {
         for (int u = 0; u < 4; ++u) k += list.first[j + u] <= (int)blockIdx.x;
     const libra_adamw_tensor_t &t = list.t[k];
     const int64_t i = (list.begin[k] + (blockIdx.x - list.first[k])) * (GROUP_BLOCKS * STATE_BLOCK) + threadIdx.x * EACH, n = t.n;
-    const bool whole = list.aligned[k] && i + EACH <= n;
+    const bool whole = i + EACH <= n;
     const int64_t block = min(i, n - 1) / STATE_BLOCK;
     Run<T, EACH> p, g;
     Run<float, EACH> w, m, v;
@@ -326,15 +335,12 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
         for (int32_t k = 0; k < count; ++k) {
             if (tensors[k].dtype != dtype || tensors[k].n == 0) continue;
             const libra_adamw_tensor_t &t = tensors[k];
-            const bool aligned = aligned_to(t.param, 16) && aligned_to(t.grad, 16) && aligned_to(t.master, 16) && aligned_to(t.first, bits8 ? 8 : 16) &&
-                                 aligned_to(t.second, bits8 ? 8 : 16);
             const int64_t all = (t.n + GROUP_BLOCKS * STATE_BLOCK - 1) / (GROUP_BLOCKS * STATE_BLOCK);
             for (int64_t begin = 0; begin < all;) {
                 if (list.count == LAUNCH_TENSORS || blocks == LAUNCH_BLOCKS)
                     if (int rc = launch()) return rc;
                 const int64_t some = std::min(all - begin, LAUNCH_BLOCKS - blocks);
                 list.t[list.count] = t;
-                list.aligned[list.count] = aligned;
                 list.first[list.count] = (int32_t)blocks;
                 list.begin[list.count++] = begin;
                 blocks += some;

@@ -191,3 +191,76 @@ def test_broadcast_and_strided_gradients():
     ref.backward()
     assert float((x.grad.double() - z.grad).abs().max()) < 2.0 ** -24 * 400
     assert not classes.requires_grad
+
+
+def test_rows_that_are_not_contiguous():
+    from paper_2506_22714_amd import autograd as ag
+    w = torch.randn(8, 6, device="cuda")
+    ids = torch.tensor([5, 0, -1, 5], device="cuda")
+    a, b = w.clone().requires_grad_(), w.clone().requires_grad_()
+    u = torch.randn(4, 8, device="cuda")
+    (ag.embedding(a.t(), ids) * u).sum().backward()
+    (ag.embedding(b.t().contiguous(), ids) * u).sum().backward()
+    assert torch.equal(a.grad, b.grad)
+    t = torch.tensor([1, 0, -1, 7, 2, 2], device="cuda")
+    a, b = w.clone().requires_grad_(), w.clone().requires_grad_()
+    for x, of in ((a, a.t()), (b, b.t().contiguous())):
+        logp, h, top, _ = ag.log_probs(of, t, top=3)
+        (logp.sum() + 2 * h.sum() + top[:, 2].sum()).backward()
+    assert torch.equal(a.grad, b.grad)
+
+
+def test_embedding_gradient_against_differences():
+    """The lookup is linear: over steps of a power of two its differences in fp32 are exact but for the roundings of scale * weight."""
+    from paper_2506_22714_amd import autograd as ag
+    w = torch.randint(-8, 9, (5, 3), device="cuda").float()
+    ids = torch.tensor([4, 1, 4, -1, 0, 4], device="cuda")
+    u = torch.randint(-4, 5, (6, 3), device="cuda").float()
+    f = lambda v: float((ag.embedding(v, ids, scale=0.5) * u).sum())        # noqa: E731
+    v = w.clone().requires_grad_()
+    (ag.embedding(v, ids, scale=0.5) * u).sum().backward()
+    for k in range(15):
+        d = torch.zeros(15, device="cuda")
+        d[k] = 2.0
+        d = d.view(5, 3)
+        assert (f(w + d) - f(w - d)) / 4 == float(v.grad.view(-1)[k])
+
+
+def test_two_streams_at_once():
+    """Calls that need a workspace, on two streams, against the same calls one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    cases = []
+    for n, rows in ((70000, 5000), (90000, 20000)):
+        ids = torch.randint(-1, rows, (n,), generator=g, device="cuda")
+        cases.append((torch.randn(n, 64, generator=g, device="cuda").half(), ids, rows, torch.randn(3, 80000 + rows, generator=g, device="cuda"),
+                      torch.randint(0, 1000, (3,), generator=g, device="cuda")))
+    def call(c):
+        return [lb.embedding_backward(c[0], c[1], c[2]), *lb.log_probs(c[3], c[4], top=7)]
+    want = [call(c) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[] for _ in cases]
+    for _ in range(5):
+        for k, (c, s) in enumerate(zip(cases, streams)):
+            with torch.cuda.stream(s):
+                got[k].append(call(c))
+    torch.cuda.synchronize()
+    for w, several in zip(want, got):
+        for one in several:
+            assert all(torch.equal(a, b) for a, b in zip(w, one))
+
+
+def test_the_optimizer_agrees_with_torch():
+    """Three steps of both; fp32 on both sides, some forty roundings of 2^-24 a step apart, of steps of 1e-2 and weights of size 4."""
+    from paper_2506_22714_amd.optim import AdamW
+    ps = [torch.nn.Parameter(torch.randn(s, device="cuda")) for s in (1000, 77)]
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    a, b = AdamW(ps, lr=1e-2, weight_decay=0.1), torch.optim.AdamW(qs, lr=1e-2, weight_decay=0.1)
+    for _ in range(3):
+        for p, q in zip(ps, qs):
+            p.grad = torch.randn_like(p)
+            q.grad = p.grad.clone()
+        a.step()
+        b.step()
+    for p, q in zip(ps, qs):
+        assert float((p - q).detach().abs().max()) < 3 * 2.0 ** -24 * (40 * 1e-2 + 2 * 5)
