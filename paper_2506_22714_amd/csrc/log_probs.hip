@@ -16,7 +16,8 @@ using namespace libra;
 namespace {
 
 constexpr float INF = __builtin_inff(), LOWEST = -0x1.fffffep127f, LOG2E = 1.44269504088896340736f;
-constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 4096 - 7, MAX_PARTS = 64;
+constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 2048 - 7, MAX_PARTS = 64;
+constexpr int64_t WAVE_CLASSES = 16384, WAVE_ROWS = 1024, WAVE_RUN_CLASSES = 8192;
 static_assert(MAX_TOP <= WAVE_LANES, "a list of the best logits has a lane for each");
 
 // NaN if one of them is
@@ -113,7 +114,7 @@ __device__ inline void write_alternative(const Forward &f, int64_t i, int a, uin
 
 // ---- short rows: L lanes hold a row in registers, E numbers each ----
 // They load the 16-byte pieces of memory that the row touches; a piece at an end of the row holds numbers of its neighbours, which count for
-// nothing.  (A load for every number where rows are not aligned: 65,536 x 500 bf16 46 us, not 22.)
+// nothing.  (A load for every number where rows are not aligned: 65,536 x 500 bf16 46 us, where these took 22.)
 template <class T> struct Span {        // of all rows, and its whole pieces
     const T *low, *high;
     const T *first, *last;              // last < first: there is none
@@ -177,7 +178,7 @@ template <> struct ShortKey<float> {
     __device__ static int64_t class_at(uint64_t key) { return class_of(key); }
 };
 
-// The best logits one after another: the best of each lane's, then of the group's; the lane that has it drops it.
+// The best logits one after another: the best of each lane's, then of the group's.  All keys of classes differ.
 template <class T, int L, int E> __device__ inline void short_alternatives(const Forward &f, const ShortRow<T, L, E> &row, int64_t i, int lane, bool there, const Finished &r) {
     typedef ShortKey<T> Key;
     typename Key::type key[E];
@@ -186,13 +187,13 @@ template <class T, int L, int E> __device__ inline void short_alternatives(const
         const int j = row.class_at(lane, e);
         key[e] = j >= 0 && j < f.classes ? Key::of(row.x[e], j) : 0;
     }
+    typename Key::type best = 0;
     for (int a = 0; a < f.top; ++a) {
-        typename Key::type best = key[0];
+        // key - best wraps round for the keys below the last best, so that the next one has the largest difference
+        typename Key::type most = key[0] - best;
 #pragma unroll
-        for (int e = 1; e < E; ++e) best = key[e] > best ? key[e] : best;
-        best = over_group<L>(best, [](auto p, auto q) { return p > q ? p : q; });
-#pragma unroll
-        for (int e = 0; e < E; ++e) key[e] = key[e] == best ? 0 : key[e];
+        for (int e = 1; e < E; ++e) most = key[e] - best > most ? key[e] - best : most;
+        best += over_group<L>(most, [](auto p, auto q) { return p > q ? p : q; });
         if (there && lane == a % L) {
             f.top_out[i * f.top + a] = r.logp(Key::logit(best), f.scale);
             f.top_index[i * f.top + a] = Key::class_at(best);
@@ -263,8 +264,8 @@ template <class F> __device__ inline void merge_lists(const uint64_t *keys, int 
     }
 }
 
-// All rows of a wave at once: 131,072 x 40 fp32 8.2 us, 65,536 x 1,000 bf16 31 us (4.3 TB/s; the exponential and the sums of 16-bit logits
-// take the vector ALUs about as long as memory).
+// All rows of a wave at once: 131,072 x 40 fp32 5.7 us (3.7 TB/s), 65,536 x 1,000 bf16 34 us (3.9 TB/s; the exponential and the sums of 16-bit
+// logits take the vector ALUs about as long as memory), fp32 of 1,000 classes 5.7 TB/s.
 template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits) {
     const int lane = threadIdx.x % L;
     const float c = f.scale * LOG2E;
@@ -310,25 +311,39 @@ struct Parts {                      // of rows that several workgroups share
     uint64_t *keys;                 // top for each
 };
 
-constexpr int LONG_THREADS = 256, LONG_WAVES = LONG_THREADS / WAVE_LANES, ROUNDS = 8;
+constexpr int LONG_THREADS = 256, ROUNDS = 8;
 
-// A thread takes 16 logits a round.  The alternatives are looked for after every eight rounds: each thread has kept the maximum of each
-// of its rounds, and if every wave has `share` maxima that reach a rank, the row has `top` logits that do, so that only the few
-// rounds of a thread that reach it are read again, a lane each, and their logits go through the list.
-// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 94 / 122 / 123 / 145 / 216; looking at every logit as it
-// comes by, with the same bound, 99 / 129 / 151 / 203 / 350, with each wave's own list as the bound 97 / 129 / 191 / 364 / 757.
-// (Two rounds in flight instead of one: 5 to 14 % slower, fewer waves fit.)
-template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_kernel(Forward f, const T *logits, Parts parts) {
-    constexpr int W = VECTOR<T>, U = 16 / W, N = U * W, ROUND = U * LONG_THREADS;
-    __shared__ float shared_sums[LONG_WAVES][3];
-    __shared__ uint64_t shared_keys[LONG_WAVES * MAX_TOP];
-    __shared__ uint32_t shared_floor[LONG_WAVES];
+// LDS of the waves of a row: what they exchange
+template <int WAVES> struct RowShared {
+    float sums[WAVES][3];
+    uint64_t keys[WAVES * MAX_TOP];
+    uint32_t floor[WAVES];
+};
+template <> struct RowShared<1> {};
+template <int WAVES> __device__ inline void row_barrier() {
+    if constexpr (WAVES > 1) __syncthreads();
+}
+// Which of the workgroup's rows this wave works on, in a scalar register, and with it all that follows from the row
+template <int WAVES> __device__ inline int row_of_wave() { return WAVES * WAVE_LANES == LONG_THREADS ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / (WAVES * WAVE_LANES)); }
+
+// WAVES waves for a row or a part of it, 4 / WAVES rows for a workgroup.  A thread takes 16 logits a round.  The alternatives are looked for
+// after every eight rounds: each thread has kept the maximum of each of its rounds, and if every wave has `share` maxima that reach a rank, the
+// row has `top` logits that do, so that only the few rounds of a thread that reach it are read again, a lane each, and their logits go
+// through the list.
+// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 99 / 115 / 118 / 135 / 194.  When this way was chosen it took
+// 94 / 122 / 123 / 145 / 216; looking at every logit as it comes by, with the same bound, 99 / 129 / 151 / 203 / 350, with each wave's own
+// list as the bound 97 / 129 / 191 / 364 / 757.  (Two rounds in flight instead of one: 5 to 14 % slower, fewer waves fit.)
+// A kernel of its own without alternatives has 63 registers, not 79 (16-bit logits): 20,000 classes 5.4 TB/s, not 5.0.  With them six waves on a
+// SIMD are asked for where that spills nothing: 16-bit logits, 12,000 classes by workgroups 3.0 TB/s, not 2.9; 32-bit ones would spill.
+template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREADS, TOP && sizeof(T) == 2 ? 6 : 1) void long_rows_kernel(Forward f, const T *logits, Parts parts) {
+    constexpr int W = VECTOR<T>, U = 16 / W, N = U * W, THREADS = WAVES * WAVE_LANES, ROUND = U * THREADS, ROWS = LONG_THREADS / THREADS;
+    __shared__ RowShared<WAVES> shared;
     __shared__ float maxima[ROUNDS][LONG_THREADS];
-    __shared__ uint16_t reaching[LONG_WAVES][ROUNDS * WAVE_LANES];
-    const int share = (f.top + LONG_WAVES - 1) / LONG_WAVES;
-    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
+    __shared__ uint16_t reaching[LONG_THREADS / WAVE_LANES][ROUNDS * WAVE_LANES];
+    const int share = (f.top + WAVES - 1) / WAVES;
+    const int lane = threadIdx.x % WAVE_LANES, in_group = threadIdx.x / WAVE_LANES, wave = in_group % WAVES, thread = threadIdx.x % THREADS;
     const float c = f.scale * LOG2E;
-    for (int64_t unit = blockIdx.x; unit < f.n * parts.count; unit += gridDim.x) {
+    for (int64_t unit = (int64_t)blockIdx.x * ROWS + row_of_wave<WAVES>(); unit < f.n * parts.count; unit += (int64_t)gridDim.x * ROWS) {
         const int64_t i = unit / parts.count;
         const int part = (int)(unit % parts.count);
         const T *x = logits + i * f.ld;
@@ -347,11 +362,11 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
             if (v0 >= end) return;
             if (v0 * W >= before && v0 + ROUND <= end && (v0 + ROUND) * W <= before + f.classes) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + (v0 + u * LONG_THREADS + threadIdx.x) * W - before);
+                for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + (v0 + u * THREADS + thread) * W - before);
                 return;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = fetch_piece(v0 + threadIdx.x + u * LONG_THREADS);
+            for (int u = 0; u < U; ++u) raw[u] = fetch_piece(v0 + thread + u * THREADS);
         };
         Sums a;
         Best best;
@@ -369,11 +384,11 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
 #pragma unroll
                 for (int k = 1; k < N; ++k) most = larger(most, y[k]);
                 a.template add<N>(y, most, c);
-                if (f.top) maxima[rounds][threadIdx.x] = most;
+                if constexpr (TOP) maxima[rounds][threadIdx.x] = most;
 #pragma unroll
                 for (int u = 0; u < U; ++u) raw[u] = next[u];
             }
-            if (!f.top) continue;
+            if constexpr (!TOP) continue;
             uint32_t rank[ROUNDS], largest = 0;
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
@@ -381,67 +396,76 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_ker
                 largest = max(largest, rank[r]);
             }
             floor = max(floor, wave_kth(largest, share));
-            if (lane == 0) shared_floor[wave] = floor;
-            __syncthreads();
-            uint32_t least = shared_floor[0];
+            uint32_t least = floor;
+            if constexpr (WAVES > 1) {
+                if (lane == 0) shared.floor[wave] = floor;
+                __syncthreads();
+                least = shared.floor[0];
 #pragma unroll
-            for (int w = 1; w < LONG_WAVES; ++w) least = min(least, shared_floor[w]);
-            // (a wave with masked classes alone, or none, shows nothing: then this wave's own)
-            if (least <= rank_of(-INF)) least = max(least, wave_kth(largest, f.top));
+                for (int w = 1; w < WAVES; ++w) least = min(least, shared.floor[w]);
+                // (a wave with masked classes alone, or none, shows nothing: then this wave's own)
+                if (least <= rank_of(-INF)) least = max(least, wave_kth(largest, f.top));
+            }
             least = max(least, (uint32_t)(best.limit >> 32));
             int many = 0;
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
                 const bool there = r < rounds && rank[r] >= least;
                 const uint64_t those = __ballot(there);
-                if (there) reaching[wave][many + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(r * WAVE_LANES + lane);
+                if (there) reaching[in_group][many + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(r * WAVE_LANES + lane);
                 many += (int)__popcll(those);
             }
             __builtin_amdgcn_wave_barrier();
             for (int q = 0; q < many; q += WAVE_LANES) {
-                const int at = reaching[wave][min(q + lane, many - 1)];
+                const int at = reaching[in_group][min(q + lane, many - 1)];
                 const int64_t v = super + (at / WAVE_LANES) * ROUND + wave * WAVE_LANES + at % WAVE_LANES;
                 // the best that these logits can be: their maximum, of the lowest class (rows of equal logits, masked ones among them, have little to read)
                 const uint32_t lowest = (uint32_t)max(v * W - before, (int64_t)0);
-                const bool there = q + lane < many && ((uint64_t)rank_of(maxima[at / WAVE_LANES][wave * WAVE_LANES + at % WAVE_LANES]) << 32 | (0xffffffffu - lowest)) > best.limit;
+                const bool there = q + lane < many && ((uint64_t)rank_of(maxima[at / WAVE_LANES][in_group * WAVE_LANES + at % WAVE_LANES]) << 32 | (0xffffffffu - lowest)) > best.limit;
                 if (!__ballot(there)) continue;
                 uint4 again[U];
                 float y[N];
 #pragma unroll
-                for (int u = 0; u < U; ++u) again[u] = fetch_piece(v + u * LONG_THREADS);
+                for (int u = 0; u < U; ++u) again[u] = fetch_piece(v + u * THREADS);
 #pragma unroll
                 for (int u = 0; u < U; ++u) unpack<T>(again[u], y + u * W);
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
-                    const int64_t p = v + (k / W) * LONG_THREADS, j = p * W + k % W - before;
+                    const int64_t p = v + (k / W) * THREADS, j = p * W + k % W - before;
                     const bool near = there && rank_of(y[k]) >= least && p < end && j >= 0 && j < f.classes;
                     if (__ballot(near)) best.insert(near ? key_of(y[k], (uint32_t)j) : 0, f.top);
                 }
             }
             floor = max(floor, (uint32_t)(read_lane(best.key, share - 1) >> 32));
-            __syncthreads();            // the bounds have been read
+            row_barrier<WAVES>();           // the bounds have been read
         }
         a = over_group_sums<WAVE_LANES>(a, c);
-        if (lane == 0) shared_sums[wave][0] = a.m, shared_sums[wave][1] = a.s, shared_sums[wave][2] = a.t;
-        if (lane < f.top) shared_keys[wave * f.top + lane] = best.key;
-        __syncthreads();
-        if (wave == 0) {
-            a = Sums{};
-            for (int w = 0; w < LONG_WAVES; ++w) a.join(Sums{shared_sums[w][0], shared_sums[w][1], shared_sums[w][2]}, c);
-            if (parts.count == 1) {
-                const Finished r = finish(a);
-                if (lane == 0) write_row(f, x, i, a, r);
-                if (f.top) merge_lists(shared_keys, LONG_WAVES, f.top, [&](int k, uint64_t key) {
-                    if (lane == 0) write_alternative(f, i, k, key, r);
-                });
-            } else {
-                if (lane == 0) parts.sums[3 * unit] = a.m, parts.sums[3 * unit + 1] = a.s, parts.sums[3 * unit + 2] = a.t;
-                if (f.top) merge_lists(shared_keys, LONG_WAVES, f.top, [&](int k, uint64_t key) {
-                    if (lane == 0) parts.keys[unit * f.top + k] = key;
-                });
+        if constexpr (WAVES == 1) {         // (never a part)
+            const Finished r = finish(a);
+            if (lane == 0) write_row(f, x, i, a, r);
+            if (TOP && lane < f.top) write_alternative(f, i, lane, best.key, r);
+        } else {
+            if (lane == 0) shared.sums[wave][0] = a.m, shared.sums[wave][1] = a.s, shared.sums[wave][2] = a.t;
+            if (TOP && lane < f.top) shared.keys[wave * f.top + lane] = best.key;
+            __syncthreads();
+            if (wave == 0) {
+                a = Sums{};
+                for (int w = 0; w < WAVES; ++w) a.join(Sums{shared.sums[w][0], shared.sums[w][1], shared.sums[w][2]}, c);
+                if (parts.count == 1) {
+                    const Finished r = finish(a);
+                    if (lane == 0) write_row(f, x, i, a, r);
+                    if (TOP) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
+                        if (lane == 0) write_alternative(f, i, k, key, r);
+                    });
+                } else {
+                    if (lane == 0) parts.sums[3 * unit] = a.m, parts.sums[3 * unit + 1] = a.s, parts.sums[3 * unit + 2] = a.t;
+                    if (TOP) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
+                        if (lane == 0) parts.keys[unit * f.top + k] = key;
+                    });
+                }
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -553,22 +577,22 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
     }
 }
 
-// A workgroup takes a run of pieces of a row; the classes that get more than p_j (...) are written a second time, whole.  Rows are
-// taken from the last to the first: the forward pass has just read the last ones.  8,191 x 32,768 bf16: 184 to 200 us, a copy of these bytes 203.
-template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
-    constexpr int W = VECTOR<T>, U = 32 / W;
-    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES;
-    for (int64_t unit = (int64_t)blockIdx.x; unit < g.n * runs; unit += gridDim.x) {
+// WAVES waves take a run of pieces of a row; the classes that get more than p_j (...) are written a second time, whole.  Rows are taken
+// from the last to the first: the forward pass has just read the last ones.  8,191 x 32,768 bf16: 184 to 200 us, a copy of these bytes 203.
+template <class T, int WAVES> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
+    constexpr int W = VECTOR<T>, U = 32 / W, THREADS = WAVES * WAVE_LANES, ROWS = LONG_THREADS / THREADS;
+    const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES % WAVES, thread = threadIdx.x % THREADS;
+    for (int64_t unit = (int64_t)blockIdx.x * ROWS + row_of_wave<WAVES>(); unit < g.n * runs; unit += (int64_t)gridDim.x * ROWS) {
         const int64_t i = g.n - 1 - unit / runs, run = unit % runs;
         const T *x = logits + i * g.ld;
         T *o = out + i * g.ld_out;
         const int before = (int)((uintptr_t)x % 16 / sizeof(T));
-        const int64_t first = run * (U * LONG_THREADS), low = first * W - before, high = low + (int64_t)U * LONG_THREADS * W;
+        const int64_t first = run * (U * THREADS), low = first * W - before, high = low + (int64_t)U * THREADS * W;
         RowGradient r;
         if (low >= 0 && high <= g.classes) {
             uint4 raw[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + low + (u * LONG_THREADS + threadIdx.x) * W);
+            for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + low + (u * THREADS + thread) * W);
             r.load<WAVE_LANES>(g, i, lane);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -576,13 +600,13 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_bac
                 unpack<T>(raw[u], y);
 #pragma unroll
                 for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
-                *reinterpret_cast<Unaligned *>(o + low + (u * LONG_THREADS + threadIdx.x) * W) = __builtin_bit_cast(Unaligned, pack<T>(y));
+                *reinterpret_cast<Unaligned *>(o + low + (u * THREADS + thread) * W) = __builtin_bit_cast(Unaligned, pack<T>(y));
             }
         } else {                                // the first and the last run of a row
             r.load<WAVE_LANES>(g, i, lane);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t j = low + (u * LONG_THREADS + threadIdx.x) * W;
+                const int64_t j = low + (u * THREADS + thread) * W;
                 float y[W];
                 if (j >= 0 && j + W <= g.classes) {
                     unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
@@ -596,20 +620,21 @@ template <class T> __global__ __launch_bounds__(LONG_THREADS) void long_rows_bac
                 }
             }
         }
-        if (r.empty || (r.target < 0 && !g.d_top)) continue;        // the same for the whole workgroup
-        __syncthreads();
-        // the first wave writes the alternatives, the second one the target unless it is among them
-        if (wave < 2) {
+        if (r.empty || (r.target < 0 && !g.d_top)) continue;        // the same for all waves of the row
+        row_barrier<WAVES>();
+        if constexpr (WAVES == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        // the alternatives by a lane each, and the target unless it is among them
+        if (wave == 0) {
             const bool listed = g.d_top && lane < g.top;
-            int64_t j = listed ? g.top_index[i * g.top + lane] : -1;
-            float more = listed && wave == 0 ? g.d_top[i * g.top + lane] + (j == r.target ? r.d : 0.f) : r.d;
-            if (wave == 1) {
-                const bool among = __ballot(listed && j == r.target) != 0;
-                j = lane == 0 && !among ? r.target : -1;
-            }
-            if (j >= 0 && j >= low && j < high && j < g.classes) o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
+            const int64_t j = listed ? g.top_index[i * g.top + lane] : -1;
+            const bool among = __ballot(listed && j == r.target) != 0;
+            auto write = [&](int64_t j, float more) {
+                if (j >= 0 && j >= low && j < high && j < g.classes) o[j] = round_to<T>(fmaf(g.scale, more, r.at(load_as_float(x[j]), g.scale)));
+            };
+            if (listed) write(j, g.d_top[i * g.top + lane] + (j == r.target ? r.d : 0.f));
+            if (lane == 0 && !among) write(r.target, r.d);
         }
-        __syncthreads();
+        row_barrier<WAVES>();
     }
 }
 
@@ -620,30 +645,43 @@ int shape(int64_t n, int64_t classes, int32_t top) {
     return LIBRA_OK;
 }
 
-// Parts of a long row: as many as keep all workgroups on the compute units at once (seven on each of 256: their registers), a part having a
-// round of loads at least.  (Rounded up to 2,048: 1,000 x 50,000 bf16 26.5 us and with 20 alternatives 51.6, not 20.8 and 36.9.)
+// A wave for a row of few rounds, if there are rows for all compute units then; otherwise a workgroup, whose waves have to wait for each other.
+// In us with 0 / 1 / 10 alternatives, bf16, by waves and by workgroups: 8,192 x 2,100 14 / 20 / 25 and 25 / 51 / 66, 8,192 x 8,192 27 / 34 / 39
+// and 28 / 51 / 66, 4,096 x 12,000 19 / 25 / 31 and 21 / 34 / 42; 1,024 x 4,000 5.1 / 8.3 / 10.2 and 5.4 / 10.3 / 13.8, but 1,024 x 12,000
+// 9.2 / 14.9 / 18.6 and 8.2 / 12.7 / 16.2, 256 x 20,000 13 / 21 / 26 and 9 / 14 / 19.
+bool wave_rows(int64_t n, int64_t classes) { return n >= WAVE_ROWS && classes <= std::min(WAVE_CLASSES, 4 * n); }
+
+// Parts of a long row: as many as keep all workgroups on the compute units at once (six on each of 256: their registers), a part having a
+// round of loads at least.  (Rounded up to 2,048: 1,000 x 50,000 bf16 26.5 us and with 20 alternatives 51.6, not 20.8 and 36.9; to 1,792: 800 x 20,000 14.1,
+// not 10.0.)
 int32_t part_count(int64_t n, int64_t classes) {
-    if (classes <= SHORT_CLASSES) return 1;
-    const int64_t wanted = 1792 / n, most = (classes + 4095) / 4096;
+    if (classes <= SHORT_CLASSES || wave_rows(n, classes)) return 1;
+    const int64_t wanted = 1536 / n, most = (classes + 4095) / 4096;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(wanted, most), MAX_PARTS));
 }
 
 size_t part_bytes(int64_t n, int32_t count, int32_t top) { return count == 1 ? 0 : ((size_t)n * count * 12 + 255) / 256 * 256 + (size_t)n * count * top * 8; }
 
-// f(lanes of a row, numbers of a lane) for rows that with their neighbours' numbers in the first piece have `numbers`
-template <class F> int for_short(int64_t numbers, F &&f) {
+// f(lanes of a row, numbers of a lane) for rows that with their neighbours' numbers in the first piece have `numbers`; a lane has EACH or
+// half as many again of rows of 17 to 768.  (Without the halves 300 classes bf16 2.5 TB/s, not 3.2, 1,100 2.3, not 3.0: idle lanes.)
+template <int EACH, class F> int for_short(int64_t numbers, F &&f) {
 #define LIBRA_SHORT(L, E) \
     if (numbers <= L * E) return f(std::integral_constant<int, L>{}, std::integral_constant<int, E>{});
     LIBRA_SHORT(1, 16)
-    LIBRA_SHORT(4, 8)
-    LIBRA_SHORT(8, 8)
-    LIBRA_SHORT(16, 8)
-    LIBRA_SHORT(32, 8)
-    LIBRA_SHORT(64, 8)
+    LIBRA_SHORT(32 / EACH, EACH)
+    if constexpr (EACH == 16) LIBRA_SHORT(2, 24)        // (three pieces for 8: 40 classes, backward, 4.3 TB/s, not 5.2)
+    LIBRA_SHORT(64 / EACH, EACH)
+    if constexpr (EACH == 16) LIBRA_SHORT(4, 24)
+    LIBRA_SHORT(128 / EACH, EACH)
+    LIBRA_SHORT(128 / EACH, EACH * 3 / 2)
+    LIBRA_SHORT(256 / EACH, EACH)
+    LIBRA_SHORT(256 / EACH, EACH * 3 / 2)
+    LIBRA_SHORT(512 / EACH, EACH)
+    LIBRA_SHORT(512 / EACH, EACH * 3 / 2)
     LIBRA_SHORT(64, 16)
-    LIBRA_SHORT(64, 32)
+    LIBRA_SHORT(64, 24)
 #undef LIBRA_SHORT
-    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
+    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 32>{});
 }
 template <class T> int64_t short_numbers(const T *x, int64_t classes, int64_t ld) { return classes + (aligned_to(x, 16) && ld % VECTOR<T> == 0 ? 0 : VECTOR<T> - 1); }
 
@@ -681,13 +719,28 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
     return for_dtype(dtype, [&](auto tag) {
         typedef decltype(tag) T;
         const T *x = (const T *)logits;
-        if (classes <= SHORT_CLASSES) return for_short(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
-            constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
-            const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
-            hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x);
-            return last_launch();
-        });
-        hipLaunchKernelGGL((long_rows_kernel<T>), dim3((unsigned)std::min<int64_t>(n * parts.count, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
+        if (classes <= SHORT_CLASSES) {
+            const int64_t numbers = short_numbers(x, classes, ld);
+            auto launch = [&](auto lanes, auto each) {
+                constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
+                const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
+                hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x);
+                return last_launch();
+            };
+            // A wave's list takes several alternatives of 32-bit logits sooner than 32 lanes with keys of 64 bits: 512 classes, 10 of them, 2.2 TB/s,
+            // not 1.6, but 4.8 without alternatives, not 5.9
+            if constexpr (sizeof(T) == 4) if (numbers > 256 && numbers <= 768 && top > 1)
+                return numbers <= 512 ? launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{})
+                                      : launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 12>{});
+            return for_short<16>(numbers, launch);
+        }
+        auto launch = [&](auto waves, auto alternatives) {
+            constexpr int WAVES = decltype(waves)::value, ROWS = LONG_THREADS / WAVE_LANES / WAVES;
+            const int64_t groups = (n * parts.count + ROWS - 1) / ROWS;
+            hipLaunchKernelGGL((long_rows_kernel<T, WAVES, decltype(alternatives)::value>), dim3((unsigned)std::min(groups, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
+        };
+        auto with = [&](auto waves) { top ? launch(waves, std::true_type{}) : launch(waves, std::false_type{}); };
+        wave_rows(n, classes) ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 4>{});
         if (parts.count > 1)
             hipLaunchKernelGGL((join_parts_kernel<T>), dim3((unsigned)std::min<int64_t>(n, MOST_WORKGROUPS)), dim3(256), (size_t)parts.count * top * 8, s, f, x, parts);
         return last_launch();
@@ -712,14 +765,22 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
         typedef decltype(tag) T;
         const T *x = (const T *)logits;
         T *o = (T *)dlogits;
-        if (classes <= SHORT_CLASSES) return for_short(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
+        // (more than 16 logits of 16 bits a lane: 1,100 classes 2.9 TB/s, not 3.3 as below; of 32 bits, where 16 bytes are four, 5.7, not 5.1)
+        if (classes <= (sizeof(T) == 2 ? SHORT_CLASSES / 2 : SHORT_CLASSES)) return for_short<2 * VECTOR<T>>(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
             const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
             hipLaunchKernelGGL((short_rows_backward_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, g, x, o);
             return last_launch();
         });
-        const int64_t pieces = (classes + 2 * VECTOR<T> - 2) / VECTOR<T>, run = 32 / VECTOR<T> * LONG_THREADS, runs = (pieces + run - 1) / run;
-        hipLaunchKernelGGL((long_rows_backward_kernel<T>), dim3((unsigned)std::min<int64_t>(n * runs, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, g, x, o, (int32_t)runs);
-        return last_launch();
+        const int64_t pieces = (classes + 2 * VECTOR<T> - 2) / VECTOR<T>;
+        auto launch = [&](auto waves) {
+            constexpr int WAVES = decltype(waves)::value, ROWS = LONG_THREADS / WAVE_LANES / WAVES;
+            const int64_t run = 32 / VECTOR<T> * WAVES * WAVE_LANES, runs = (pieces + run - 1) / run;
+            hipLaunchKernelGGL((long_rows_backward_kernel<T, WAVES>), dim3((unsigned)std::min<int64_t>((n * runs + ROWS - 1) / ROWS, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, g, x, o,
+                               (int32_t)runs);
+            return last_launch();
+        };
+        // (a workgroup's run is 8,192 logits: of shorter rows most of it would be idle)
+        return classes <= WAVE_RUN_CLASSES ? launch(std::integral_constant<int, 1>{}) : launch(std::integral_constant<int, 4>{});
     });
 }
