@@ -529,7 +529,8 @@ struct RowGradient {
     }
     __device__ float at(float x, float scale) const {
         const float logp = fmaf(scale, x - m, -logs), p = __builtin_amdgcn_exp2f(logp * LOG2E);
-        return empty ? 0.f : p * fmaf(b, fmaxf(logp, LOWEST), a);      // a masked class: p = 0; NaN comes with p
+        // p = 0 below -104, for masked classes too, where b log p must not become infinite; NaN comes with p
+        return empty ? 0.f : p * fmaf(b, fmaxf(logp, -128.f), a);
     }
 };
 

@@ -157,6 +157,86 @@ def test_masks(dtype, classes):
         check(x, t, top, 0.5)
 
 
+def of_all_kinds(n, classes, dtype, seed):
+    """Rows of ordinary logits, equal ones, ascending ones, masked ones (half, all but one, all), of the lowest number, with a NaN and infinities."""
+    x = logits(n, classes, dtype, seed=seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    kind = torch.arange(n, device="cuda") % 11
+    x[kind == 1] = 0.25
+    x[kind == 2] = torch.arange(classes, device="cuda").clamp(max=2000).to(dtype) / 64
+    x[kind == 3] = torch.randint(-2, 3, (int((kind == 3).sum()), classes), generator=g, device="cuda").to(dtype)
+    x[(kind == 4)[:, None] & (torch.rand(n, classes, generator=g, device="cuda") < 0.5)] = -INF
+    x[kind == 5] = -INF
+    x[(kind == 5), torch.randint(classes, (int((kind == 5).sum()),), generator=g, device="cuda")] = 1.5
+    x[kind == 6] = -INF
+    x[(kind == 7)[:, None] & (torch.rand(n, classes, generator=g, device="cuda") < 0.9)] = torch.finfo(dtype).min
+    x[(kind == 8) & (torch.arange(n, device="cuda") % 2 == 0), classes // 3] = float("nan")
+    x[kind == 9, classes // 2:] = -INF
+    return x
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,classes", [(6, 3), (6, 300), (6, 1500), (1040, 2500), (6, 5000), (6, 90000)])
+@pytest.mark.parametrize("e", [1.0, -2.5, 1e6])
+def test_masked_classes_have_no_gradient_of_the_entropy(dtype, n, classes, e):
+    """However large the entropy's gradient is: p log p is 0 there, not 0 times infinity."""
+    x = logits(n, classes, dtype, seed=4, spread=1.0)
+    masked = torch.rand(n, classes, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") < 0.4
+    masked[:, 0] = False
+    x[masked & (torch.arange(n, device="cuda") % 2 == 0)[:, None]] = -INF
+    x[masked & (torch.arange(n, device="cuda") % 2 == 1)[:, None]] = torch.finfo(dtype).min
+    t = torch.zeros(n, dtype=torch.int64, device="cuda")
+    r = lb.log_probs(x, t, top=1)
+    g = lb.log_probs_backward(x, r, t, torch.ones(n, device="cuda"), torch.full((n,), e, device="cuda"))
+    assert bool((g[masked] == 0).all()) and bool((g.isfinite() | (g.abs() > torch.finfo(dtype).max)).all()) and not bool(g.isnan().any())
+    assert bool((g[:, 1:][~masked[:, 1:]] != 0).any()) or classes == 3
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,classes,top", [(1023, 2042, 5), (1024, 2042, 0), (1024, 4096, 64), (1031, 4097, 3), (1030, 2053, 1), (1100, 3000, 20), (2053, 8201, 10)])
+def test_many_rows(dtype, n, classes, top):
+    """As many rows as get a wave each, and one fewer."""
+    x = of_all_kinds(n, classes, dtype, seed=classes)
+    odd = torch.isnan(x).any(1)
+    good = x[~odd]
+    check(good, targets_of(len(good), classes), top, 0.7)
+    # a NaN stays in its row.  (The other rows at the same addresses: the order of a row's sums goes by its 16-byte pieces.)
+    t = targets_of(n, classes, seed=3)
+    r, without = lb.log_probs(x, t, top=top, scale=0.7), lb.log_probs(x.nan_to_num(nan=0.0, posinf=INF, neginf=-INF), t, top=top, scale=0.7)
+    for got, want in zip(r, without):
+        assert got is want is None or torch.equal(got[~odd], want[~odd])
+    assert bool(r.entropy[odd].isnan().all()) and bool(r.target[odd & (t != -1)].isnan().all())
+    if top:
+        assert bool((r.top_index[odd, 0] == classes // 3).all()) and bool(r.top[odd].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("ld,offset", [(0, 0), (1, 0), (8, 3)])
+def test_sizes_at_which_the_way_changes(dtype, ld, offset):
+    for classes in (16, 17, 32, 33, 41, 48, 49, 64, 65, 96, 97, 128, 129, 192, 193, 256, 257, 384, 385, 512, 513, 768, 769, 1017, 1018, 1024, 1025, 1529, 1536, 1537, 2041, 2042):
+        n = 23
+        held = torch.full((offset + n * (classes + ld),), 7.0, dtype=dtype, device="cuda")
+        x = torch.as_strided(held, (n, classes), (classes + ld, 1), offset)
+        x.copy_(of_all_kinds(n, classes, dtype, seed=classes).nan_to_num(nan=1.0, posinf=3.0, neginf=-INF))
+        for top in (2, min(classes, 40)):
+            check(x, targets_of(n, classes, seed=top), top, 1.0)
+
+
+def test_many_rows_with_space_between_them():
+    """The gradient of rows of a wave each leaves what lies between its rows."""
+    n, classes, ld = 1500, 2501, 2507
+    held = logits(n, ld, torch.bfloat16, seed=5)
+    x, t = held[:, 3:3 + classes], targets_of(n, classes)
+    out = torch.full((n, ld + 4), 9.0, dtype=torch.bfloat16, device="cuda")
+    r = lb.log_probs(x, t, top=3)
+    d, e, a = (torch.randn(n, device="cuda"), torch.randn(n, device="cuda"), torch.randn(n, 3, device="cuda"))
+    lb.log_probs_backward(x, r, t, d, e, a, out=out[:, 1:1 + classes])
+    tight = lb.log_probs_backward(x.contiguous(), r, t, d, e, a)      # (with these sums: theirs would go by other 16-byte pieces)
+    check(x, t, 3, 1.0)
+    assert torch.equal(out[:, 1:1 + classes], tight)
+    assert bool((out[:, :1] == 9).all()) and bool((out[:, 1 + classes:] == 9).all())
+
+
 @pytest.mark.parametrize("classes", [5, 300, 5000])
 def test_nan_and_infinity_spoil_their_row_alone(classes):
     x = logits(6, classes, torch.float32)
