@@ -17,7 +17,7 @@ namespace {
 
 constexpr float INF = __builtin_inff(), LOWEST = -0x1.fffffep127f, LOG2E = 1.44269504088896340736f;
 constexpr int MAX_TOP = LIBRA_LOG_PROBS_MAX_TOP, SHORT_CLASSES = 2048 - 7, MAX_PARTS = 64;
-constexpr int64_t WAVE_CLASSES = 16384, WAVE_ROWS = 1024, WAVE_RUN_CLASSES = 8192;
+constexpr int64_t WAVE_CLASSES = 16384, WAVE_ROWS = 1024;
 static_assert(MAX_TOP <= WAVE_LANES, "a list of the best logits has a lane for each");
 
 // NaN if one of them is
@@ -578,8 +578,9 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
     }
 }
 
-// WAVES waves take a run of pieces of a row; the classes that get more than p_j (...) are written a second time, whole.  Rows are taken
-// from the last to the first: the forward pass has just read the last ones.  8,191 x 32,768 bf16: 184 to 200 us, a copy of these bytes 203.
+// WAVES waves take a run of pieces of a row; the target and the alternatives, which get more than p_j times a sum, are written a second time,
+// whole.  Rows are taken from the last to the first: the forward pass has just read the last ones.  8,191 x 32,768 bf16: 185 us, a copy of
+// these bytes 203.  (The ends of a row with a load for every piece and number in a branch: 2,677 classes bf16 3.1 TB/s, not 5.1.)
 template <class T, int WAVES> __global__ __launch_bounds__(LONG_THREADS) void long_rows_backward_kernel(Backward g, const T *logits, T *out, int32_t runs) {
     constexpr int W = VECTOR<T>, U = 32 / W, THREADS = WAVES * WAVE_LANES, ROWS = LONG_THREADS / THREADS;
     const int lane = threadIdx.x % WAVE_LANES, wave = threadIdx.x / WAVE_LANES % WAVES, thread = threadIdx.x % THREADS;
@@ -603,21 +604,30 @@ template <class T, int WAVES> __global__ __launch_bounds__(LONG_THREADS) void lo
                 for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
                 *reinterpret_cast<Unaligned *>(o + low + (u * THREADS + thread) * W) = __builtin_bit_cast(Unaligned, pack<T>(y));
             }
-        } else {                                // the first and the last run of a row
+        } else {
+            // the first and the last run of a row: a piece that it shares with its neighbours is loaded from where it is the row's alone, and
+            // what belongs to it is stored element by element
+            uint4 raw[U];
+            int64_t c[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                c[u] = min(max(low + (u * THREADS + thread) * W, (int64_t)0), g.classes - W);
+                if (low + u * THREADS * W < g.classes) raw[u] = __builtin_bit_cast(uint4, *reinterpret_cast<const Unaligned *>(x + c[u]));
+            }
             r.load<WAVE_LANES>(g, i, lane);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (low + u * THREADS * W >= g.classes) break;
                 const int64_t j = low + (u * THREADS + thread) * W;
                 float y[W];
-                if (j >= 0 && j + W <= g.classes) {
-                    unpack<T>(*reinterpret_cast<const uint4 *>(x + j), y);
+                unpack<T>(raw[u], y);
 #pragma unroll
-                    for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
-                    *reinterpret_cast<Unaligned *>(o + j) = __builtin_bit_cast(Unaligned, pack<T>(y));
-                } else {
+                for (int k = 0; k < W; ++k) y[k] = r.at(y[k], g.scale);
+                if (j == c[u]) *reinterpret_cast<Unaligned *>(o + j) = __builtin_bit_cast(Unaligned, pack<T>(y));
+                else {
 #pragma unroll
                     for (int k = 0; k < W; ++k)
-                        if (j + k >= 0 && j + k < g.classes) o[j + k] = round_to<T>(r.at(load_as_float(x[j + k]), g.scale));
+                        if (c[u] + k >= j && c[u] + k < j + W) o[c[u] + k] = round_to<T>(y[k]);
                 }
             }
         }
@@ -766,8 +776,8 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
         typedef decltype(tag) T;
         const T *x = (const T *)logits;
         T *o = (T *)dlogits;
-        // (more than 16 logits of 16 bits a lane: 1,100 classes 2.9 TB/s, not 3.3 as below; of 32 bits, where 16 bytes are four, 5.7, not 5.1)
-        if (classes <= (sizeof(T) == 2 ? SHORT_CLASSES / 2 : SHORT_CLASSES)) return for_short<2 * VECTOR<T>>(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
+        // (with more than 16 logits a lane fewer waves fit: 1,100 classes bf16 2.9 TB/s, not 4.3 as below; 768 classes 5.1, not 4.2)
+        if (classes <= SHORT_CLASSES / 2) return for_short<2 * VECTOR<T>>(short_numbers(x, classes, ld), [&](auto lanes, auto each) {
             constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
             const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
             hipLaunchKernelGGL((short_rows_backward_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, g, x, o);
@@ -781,7 +791,8 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
                                (int32_t)runs);
             return last_launch();
         };
-        // (a workgroup's run is 8,192 logits: of shorter rows most of it would be idle)
-        return classes <= WAVE_RUN_CLASSES ? launch(std::integral_constant<int, 1>{}) : launch(std::integral_constant<int, 4>{});
+        // (a workgroup's run is 8,192 logits, of which a row that ends in the middle leaves much idle: 12,003 classes bf16 4.5 TB/s, not 5.7; in
+        // long rows the loads of what a row has are shared: 131,072 with 10 alternatives 5.7, not 5.3)
+        return classes <= WAVE_CLASSES ? launch(std::integral_constant<int, 1>{}) : launch(std::integral_constant<int, 4>{});
     });
 }
