@@ -347,39 +347,44 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
         const int64_t i = unit / parts.count;
         const int part = (int)(unit % parts.count);
         const T *x = logits + i * f.ld;
-        // 16-byte pieces of memory: the first and the last may hold other things beside the row
+        // 16-byte pieces of memory.  The first and the last, which hold other things beside the row, are loaded from where all is the row's; so is
+        // what lies behind: every lane loads.  The numbers of other pieces are left out when they come.
         const int before = (int)((uintptr_t)x % 16 / sizeof(T));
-        const int64_t pieces = (before + f.classes + W - 1) / W, each = (pieces + parts.count - 1) / parts.count, begin = part * each, end = min(pieces, begin + each);
-        auto fetch_piece = [&](int64_t p) {
-            const int64_t j = p * W - before;
-            if (p < end && j >= 0 && j + W <= f.classes) return *reinterpret_cast<const uint4 *>(x + j);
-            float y[W];
-#pragma unroll
-            for (int k = 0; k < W; ++k) y[k] = p < end && j + k >= 0 && j + k < f.classes ? load_as_float(x[j + k]) : -INF;
-            return pack<T>(y);
-        };
-        auto fetch = [&](int64_t v0, uint4 *raw) {
+        const int32_t pieces = (int32_t)((before + f.classes + W - 1) / W), each = (pieces + parts.count - 1) / parts.count, begin = part * each, end = min(pieces, begin + each);
+        const int32_t first_whole = before ? 1 : 0, last_whole = min(end, (int32_t)((before + f.classes) / W)) - ROUND;
+        auto class_of_piece = [&](int32_t p) { return min(max((int64_t)p * W - before, (int64_t)0), f.classes - W); };
+        auto is_of_piece = [&](int32_t p, int64_t j) { return p < end && j >= (int64_t)p * W - before && j < (int64_t)p * W - before + W; };
+        auto inside = [&](int32_t v0) { return v0 >= first_whole && v0 <= last_whole; };
+        auto fetch = [&](int32_t v0, uint4 *raw) {
             if (v0 >= end) return;
-            if (v0 * W >= before && v0 + ROUND <= end && (v0 + ROUND) * W <= before + f.classes) {
+            if (inside(v0)) {
+                const uint4 *from = reinterpret_cast<const uint4 *>(x - before) + v0;
 #pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = *reinterpret_cast<const uint4 *>(x + (v0 + u * THREADS + thread) * W - before);
+                for (int u = 0; u < U; ++u) raw[u] = from[u * THREADS + thread];
                 return;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = fetch_piece(v0 + thread + u * THREADS);
+            for (int u = 0; u < U; ++u) raw[u] = __builtin_bit_cast(uint4, *reinterpret_cast<const Unaligned *>(x + class_of_piece(v0 + thread + u * THREADS)));
         };
         Sums a;
         Best best;
         uint32_t floor = 0;             // what this wave has shown of the row
         uint4 raw[U], next[U];
         fetch(begin, raw);
-        for (int64_t super = begin; super < end; super += ROUNDS * ROUND) {
+        for (int32_t super = begin; super < end; super += ROUNDS * ROUND) {
             int rounds = 0;
-            for (int64_t v0 = super; rounds < ROUNDS && v0 < end; v0 += ROUND, ++rounds) {
+            for (int32_t v0 = super; rounds < ROUNDS && v0 < end; v0 += ROUND, ++rounds) {
                 fetch(v0 + ROUND, next);                // on its way while this one is worked on
                 float y[N];
 #pragma unroll
                 for (int u = 0; u < U; ++u) unpack<T>(raw[u], y + u * W);
+                if (!inside(v0)) {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const int32_t p = v0 + thread + (k / W) * THREADS;
+                        if (!is_of_piece(p, class_of_piece(p) + k % W)) y[k] = -INF;
+                    }
+                }
                 float most = y[0];
 #pragma unroll
                 for (int k = 1; k < N; ++k) most = larger(most, y[k]);
@@ -418,21 +423,22 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
             __builtin_amdgcn_wave_barrier();
             for (int q = 0; q < many; q += WAVE_LANES) {
                 const int at = reaching[in_group][min(q + lane, many - 1)];
-                const int64_t v = super + (at / WAVE_LANES) * ROUND + wave * WAVE_LANES + at % WAVE_LANES;
+                const int32_t v = super + (at / WAVE_LANES) * ROUND + wave * WAVE_LANES + at % WAVE_LANES;
                 // the best that these logits can be: their maximum, of the lowest class (rows of equal logits, masked ones among them, have little to read)
-                const uint32_t lowest = (uint32_t)max(v * W - before, (int64_t)0);
+                const uint32_t lowest = (uint32_t)max((int64_t)v * W - before, (int64_t)0);
                 const bool there = q + lane < many && ((uint64_t)rank_of(maxima[at / WAVE_LANES][in_group * WAVE_LANES + at % WAVE_LANES]) << 32 | (0xffffffffu - lowest)) > best.limit;
                 if (!__ballot(there)) continue;
                 uint4 again[U];
                 float y[N];
 #pragma unroll
-                for (int u = 0; u < U; ++u) again[u] = fetch_piece(v + u * THREADS);
+                for (int u = 0; u < U; ++u) again[u] = __builtin_bit_cast(uint4, *reinterpret_cast<const Unaligned *>(x + class_of_piece(v + u * THREADS)));
 #pragma unroll
                 for (int u = 0; u < U; ++u) unpack<T>(again[u], y + u * W);
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
-                    const int64_t p = v + (k / W) * THREADS, j = p * W + k % W - before;
-                    const bool near = there && rank_of(y[k]) >= least && p < end && j >= 0 && j < f.classes;
+                    const int32_t p = v + (k / W) * THREADS;
+                    const int64_t j = class_of_piece(p) + k % W;
+                    const bool near = there && rank_of(y[k]) >= least && is_of_piece(p, j);
                     if (__ballot(near)) best.insert(near ? key_of(y[k], (uint32_t)j) : 0, f.top);
                 }
             }
