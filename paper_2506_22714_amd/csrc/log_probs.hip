@@ -201,6 +201,33 @@ template <class T, int L, int E> __device__ inline void short_alternatives(const
     }
 }
 
+// What lane (this ^ MASK) holds
+template <int MASK> __device__ inline uint32_t lane_xor(uint32_t x) {
+    if constexpr (MASK == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true);             // quad_perm [1,0,3,2]
+    else if constexpr (MASK == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true);        // quad_perm [2,3,0,1]
+    else if constexpr (MASK == 3) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x1B, 0xf, 0xf, true);        // quad_perm [3,2,1,0]
+    else if constexpr (MASK == 4) return lane_xor<7>(lane_xor<3>(x));
+    else if constexpr (MASK == 7) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true);       // row_half_mirror
+    else if constexpr (MASK == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);       // row_ror:8
+    else if constexpr (MASK == 15) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true);      // row_mirror
+    else return (uint32_t)__shfl_xor((int)x, MASK);
+}
+// The larger of the two in the lower lane, the smaller one in the upper
+template <int MASK> __device__ inline uint64_t ordered(uint64_t x) {
+    const uint64_t other = (uint64_t)lane_xor<MASK>((uint32_t)(x >> 32)) << 32 | lane_xor<MASK>((uint32_t)x);
+    const bool upper = ((int)(threadIdx.x % WAVE_LANES) ^ MASK) < (int)(threadIdx.x % WAVE_LANES);
+    return (x > other) != upper ? x : other;
+}
+// A wave's keys into descending order if every half of L lanes is: the halves' pairs from outside in, then smaller and smaller halves
+template <int L> __device__ inline uint64_t cleaned(uint64_t x) {
+    if constexpr (L == 1) return x;
+    else return cleaned<L / 2>(ordered<L / 2>(x));
+}
+template <int L> __device__ inline uint64_t sorted(uint64_t x) {
+    if constexpr (L == 1) return x;
+    else return cleaned<L / 2>(ordered<L - 1>(sorted<L / 2>(x)));
+}
+
 // The best logits that a wave has seen, in descending order, one in each of the first `top` lanes.
 struct Best {
     uint64_t key = 0;               // this lane's
@@ -221,8 +248,44 @@ struct Best {
             limit = read_lane(key, top - 1);
         }
     }
+    // All of them at once: of two descending lists, one turned round, the larger of each pair of lanes are the best 64, rising and falling once
+    __device__ void join(uint64_t brought, int top) {
+        const uint64_t x = sorted<WAVE_LANES>(brought), turned = (uint64_t)lane_xor<63>((uint32_t)(x >> 32)) << 32 | lane_xor<63>((uint32_t)x);
+        key = cleaned<WAVE_LANES>(key > turned ? key : turned);
+        limit = read_lane(key, top - 1);
+    }
 };
 
+// Logits on their way into a wave's list: one by one, or up to 64 in LDS and then sorted, for a wave with a whole row and a long list.
+// Inserting takes some 14 instructions for each, sorting 64 and joining them 230.  65,536 x 1,000 bf16 with 10 / 20 / 64 alternatives
+// 76 / 117 / 496 us one by one, 89 / 96 / 226 sorted.  (One kernel with both: 10 % slower where few are asked for.)
+constexpr int SORTED_TOP = 14;
+template <bool SORTED> struct Waiting {
+    uint64_t *keys;                 // of this wave
+    int many = 0;
+    __device__ void add(bool near, uint64_t key, Best &best, int top) {
+        const uint64_t those = __ballot(near);
+        if (!those) return;
+        if constexpr (SORTED) {
+            const int more = (int)__popcll(those);
+            if (many + more > WAVE_LANES) flush(best, top);
+            if (near) keys[many + __popcll(those & ((1ull << (threadIdx.x % WAVE_LANES)) - 1))] = key;
+            many += more;
+        } else best.insert(near ? key : 0, top);
+    }
+    __device__ void flush(Best &best, int top) {
+        if constexpr (SORTED) {
+            if (!many) return;
+            __builtin_amdgcn_wave_barrier();            // a wave's LDS accesses keep their order
+            const int lane = threadIdx.x % WAVE_LANES;
+            const uint64_t brought = lane < many ? keys[lane] : 0;
+            __builtin_amdgcn_wave_barrier();
+            if (many > SORTED_TOP) best.join(brought, top);
+            else best.insert(brought, top);
+            many = 0;
+        }
+    }
+};
 
 // The largest rank of the wave, in a scalar register
 __device__ inline uint32_t wave_most(uint32_t x) {
@@ -266,7 +329,7 @@ template <class F> __device__ inline void merge_lists(const uint64_t *keys, int 
 
 // All rows of a wave at once: 131,072 x 40 fp32 5.7 us (3.7 TB/s), 65,536 x 1,000 bf16 34 us (3.9 TB/s; the exponential and the sums of 16-bit
 // logits take the vector ALUs about as long as memory), fp32 of 1,000 classes 5.7 TB/s.
-template <class T, int L, int E> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits) {
+template <class T, int L, int E, bool SORTED> __global__ __launch_bounds__(256) void short_rows_kernel(Forward f, const T *logits) {
     const int lane = threadIdx.x % L;
     const float c = f.scale * LOG2E;
     const Span<T> span(logits, f.n, f.classes, f.ld);
@@ -290,15 +353,18 @@ template <class T, int L, int E> __global__ __launch_bounds__(256) void short_ro
             if (f.top) short_alternatives(f, row, i, lane, there, r);
         } else if (f.top) {
             // `top` lanes have a maximum that reaches this rank: no logit below it is among the alternatives, and few others reach it.
-            // (One after another, as for shorter rows: 65,536 x 1,000 bf16 with 20 251 us, not 117.)
+            // (One after another, as for shorter rows: 65,536 x 1,000 bf16 with 20 251 us, not 96.)
+            __shared__ uint64_t keys[SORTED ? 256 / WAVE_LANES : 1][WAVE_LANES];
             const float limit = logit_of(wave_kth(rank_of(mine), f.top));
             Best best;
+            Waiting<SORTED> waiting{keys[SORTED ? threadIdx.x / WAVE_LANES : 0]};
 #pragma unroll
             for (int e = E - 1; e >= 0; --e) {
                 const int j = row.class_at(lane, e);
                 const bool near = !(row.x[e] < limit) && j >= 0 && j < f.classes;
-                if (__ballot(near)) best.insert(near ? key_of(row.x[e], (uint32_t)j) : 0, f.top);
+                waiting.add(near, key_of(row.x[e], (uint32_t)j), best, f.top);
             }
+            waiting.flush(best, f.top);
             if (there && lane < f.top) write_alternative(f, i, lane, best.key, r);
         }
     }
@@ -312,6 +378,7 @@ struct Parts {                      // of rows that several workgroups share
 };
 
 constexpr int LONG_THREADS = 256, ROUNDS = 8;
+enum List { NONE, ONE_BY_ONE, SORTED };      // how the alternatives come
 
 // LDS of the waves of a row: what they exchange
 template <int WAVES> struct RowShared {
@@ -330,16 +397,17 @@ template <int WAVES> __device__ inline int row_of_wave() { return WAVES * WAVE_L
 // after every eight rounds: each thread has kept the maximum of each of its rounds, and if every wave has `share` maxima that reach a rank, the
 // row has `top` logits that do, so that only the few rounds of a thread that reach it are read again, a lane each, and their logits go
 // through the list.
-// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 99 / 115 / 118 / 135 / 194.  When this way was chosen it took
+// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 100 / 117 / 120 / 140 / 199.  When this way was chosen it took
 // 94 / 122 / 123 / 145 / 216; looking at every logit as it comes by, with the same bound, 99 / 129 / 151 / 203 / 350, with each wave's own
 // list as the bound 97 / 129 / 191 / 364 / 757.  (Two rounds in flight instead of one: 5 to 14 % slower, fewer waves fit.)
-// A kernel of its own without alternatives has 63 registers, not 79 (16-bit logits): 20,000 classes 5.4 TB/s, not 5.0.  With them six waves on a
+// A kernel of its own without alternatives has 60 registers, not 79 (16-bit logits): 20,000 classes 5.4 TB/s, not 5.0.  With them six waves on a
 // SIMD are asked for where that spills nothing: 16-bit logits, 12,000 classes by workgroups 3.0 TB/s, not 2.9; 32-bit ones would spill.
-template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREADS, TOP && sizeof(T) == 2 ? 6 : 1) void long_rows_kernel(Forward f, const T *logits, Parts parts) {
+template <class T, int WAVES, List LIST> __global__ __launch_bounds__(LONG_THREADS, LIST != NONE && sizeof(T) == 2 ? 6 : 1) void long_rows_kernel(Forward f, const T *logits, Parts parts) {
     constexpr int W = VECTOR<T>, U = 16 / W, N = U * W, THREADS = WAVES * WAVE_LANES, ROUND = U * THREADS, ROWS = LONG_THREADS / THREADS;
     __shared__ RowShared<WAVES> shared;
     __shared__ float maxima[ROUNDS][LONG_THREADS];
     __shared__ uint16_t reaching[LONG_THREADS / WAVE_LANES][ROUNDS * WAVE_LANES];
+    __shared__ uint64_t keys[LIST == SORTED ? LONG_THREADS / WAVE_LANES : 1][WAVE_LANES];
     const int share = (f.top + WAVES - 1) / WAVES;
     const int lane = threadIdx.x % WAVE_LANES, in_group = threadIdx.x / WAVE_LANES, wave = in_group % WAVES, thread = threadIdx.x % THREADS;
     const float c = f.scale * LOG2E;
@@ -368,6 +436,7 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
         };
         Sums a;
         Best best;
+        Waiting<LIST == SORTED> waiting{keys[LIST == SORTED ? in_group : 0]};
         uint32_t floor = 0;             // what this wave has shown of the row
         uint4 raw[U], next[U];
         fetch(begin, raw);
@@ -389,11 +458,11 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
 #pragma unroll
                 for (int k = 1; k < N; ++k) most = larger(most, y[k]);
                 a.template add<N>(y, most, c);
-                if constexpr (TOP) maxima[rounds][threadIdx.x] = most;
+                if constexpr (LIST != NONE) maxima[rounds][threadIdx.x] = most;
 #pragma unroll
                 for (int u = 0; u < U; ++u) raw[u] = next[u];
             }
-            if constexpr (!TOP) continue;
+            if constexpr (LIST == NONE) continue;
             uint32_t rank[ROUNDS], largest = 0;
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
@@ -439,9 +508,10 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
                     const int32_t p = v + (k / W) * THREADS;
                     const int64_t j = class_of_piece(p) + k % W;
                     const bool near = there && rank_of(y[k]) >= least && is_of_piece(p, j);
-                    if (__ballot(near)) best.insert(near ? key_of(y[k], (uint32_t)j) : 0, f.top);
+                    waiting.add(near, key_of(y[k], (uint32_t)j), best, f.top);
                 }
             }
+            waiting.flush(best, f.top);
             floor = max(floor, (uint32_t)(read_lane(best.key, share - 1) >> 32));
             row_barrier<WAVES>();           // the bounds have been read
         }
@@ -449,10 +519,10 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
         if constexpr (WAVES == 1) {         // (never a part)
             const Finished r = finish(a);
             if (lane == 0) write_row(f, x, i, a, r);
-            if (TOP && lane < f.top) write_alternative(f, i, lane, best.key, r);
+            if (LIST != NONE && lane < f.top) write_alternative(f, i, lane, best.key, r);
         } else {
             if (lane == 0) shared.sums[wave][0] = a.m, shared.sums[wave][1] = a.s, shared.sums[wave][2] = a.t;
-            if (TOP && lane < f.top) shared.keys[wave * f.top + lane] = best.key;
+            if (LIST != NONE && lane < f.top) shared.keys[wave * f.top + lane] = best.key;
             __syncthreads();
             if (wave == 0) {
                 a = Sums{};
@@ -460,12 +530,12 @@ template <class T, int WAVES, bool TOP> __global__ __launch_bounds__(LONG_THREAD
                 if (parts.count == 1) {
                     const Finished r = finish(a);
                     if (lane == 0) write_row(f, x, i, a, r);
-                    if (TOP) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
+                    if (LIST != NONE) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
                         if (lane == 0) write_alternative(f, i, k, key, r);
                     });
                 } else {
                     if (lane == 0) parts.sums[3 * unit] = a.m, parts.sums[3 * unit + 1] = a.s, parts.sums[3 * unit + 2] = a.t;
-                    if (TOP) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
+                    if (LIST != NONE) merge_lists(shared.keys, WAVES, f.top, [&](int k, uint64_t key) {
                         if (lane == 0) parts.keys[unit * f.top + k] = key;
                     });
                 }
@@ -741,7 +811,11 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
             auto launch = [&](auto lanes, auto each) {
                 constexpr int L = decltype(lanes)::value, E = decltype(each)::value;
                 const unsigned blocks = (unsigned)std::min<int64_t>((n * L + 255) / 256, MOST_WORKGROUPS);
-                hipLaunchKernelGGL((short_rows_kernel<T, L, E>), dim3(blocks), dim3(256), 0, s, f, x);
+                if constexpr (L == WAVE_LANES) if (top > SORTED_TOP) {
+                    hipLaunchKernelGGL((short_rows_kernel<T, L, E, true>), dim3(blocks), dim3(256), 0, s, f, x);
+                    return last_launch();
+                }
+                hipLaunchKernelGGL((short_rows_kernel<T, L, E, false>), dim3(blocks), dim3(256), 0, s, f, x);
                 return last_launch();
             };
             // A wave's list takes several alternatives of 32-bit logits sooner than 32 lanes with keys of 64 bits: 512 classes, 10 of them, 2.2 TB/s,
@@ -751,13 +825,18 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
                                       : launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 12>{});
             return for_short<16>(numbers, launch);
         }
-        auto launch = [&](auto waves, auto alternatives) {
+        auto launch = [&](auto waves, auto list) {
             constexpr int WAVES = decltype(waves)::value, ROWS = LONG_THREADS / WAVE_LANES / WAVES;
             const int64_t groups = (n * parts.count + ROWS - 1) / ROWS;
-            hipLaunchKernelGGL((long_rows_kernel<T, WAVES, decltype(alternatives)::value>), dim3((unsigned)std::min(groups, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
+            hipLaunchKernelGGL((long_rows_kernel<T, WAVES, decltype(list)::value>), dim3((unsigned)std::min(groups, MOST_WORKGROUPS)), dim3(LONG_THREADS), 0, s, f, x, parts);
         };
-        auto with = [&](auto waves) { top ? launch(waves, std::true_type{}) : launch(waves, std::false_type{}); };
-        wave_rows(n, classes) ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 4>{});
+        const std::integral_constant<int, 1> wave;
+        const std::integral_constant<int, 4> workgroup;
+        const std::integral_constant<List, NONE> none;
+        const std::integral_constant<List, ONE_BY_ONE> one_by_one;
+        if (!wave_rows(n, classes)) top ? launch(workgroup, one_by_one) : launch(workgroup, none);
+        else if (top > SORTED_TOP) launch(wave, std::integral_constant<List, SORTED>{});
+        else top ? launch(wave, one_by_one) : launch(wave, none);
         if (parts.count > 1)
             hipLaunchKernelGGL((join_parts_kernel<T>), dim3((unsigned)std::min<int64_t>(n, MOST_WORKGROUPS)), dim3(256), (size_t)parts.count * top * 8, s, f, x, parts);
         return last_launch();
