@@ -2,6 +2,7 @@
 //   out[i] = scale * table[index[i]]            dtable[v] = scale * sum over i with index[i] = v of dout[i]
 // Both are bound by memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "ends.h"
 
@@ -19,11 +20,18 @@ template <class T, int ACCESS> struct Piece {
     float x[W];
     // where the piece that a row of `width` elements has at `at`, a multiple of W below the width, begins
     __device__ static int32_t column(int32_t at, int32_t width) { return ACCESS == ANYWHERE ? min(at, width - W) : at; }
-    __device__ void load(const T *p) {
-        if constexpr (ACCESS == ALIGNED) unpack<T>(*reinterpret_cast<const uint4 *>(p), x);
-        else if constexpr (ACCESS == ANYWHERE) unpack<T>(__builtin_bit_cast(uint4, *reinterpret_cast<const Unaligned *>(p)), x);
-        else x[0] = load_as_float(p[0]);
+    // as it is in memory
+    typedef std::conditional_t<ACCESS == ELEMENTS, T, uint4> Stored;
+    __device__ static Stored fetch(const T *p) {
+        if constexpr (ACCESS == ALIGNED) return *reinterpret_cast<const uint4 *>(p);
+        else if constexpr (ACCESS == ANYWHERE) return __builtin_bit_cast(uint4, *reinterpret_cast<const Unaligned *>(p));
+        else return p[0];
     }
+    __device__ void take(Stored s) {
+        if constexpr (ACCESS == ELEMENTS) x[0] = load_as_float(s);
+        else unpack<T>(s, x);
+    }
+    __device__ void load(const T *p) { take(fetch(p)); }
     __device__ void store(T *p) const {
         if constexpr (ACCESS == ALIGNED) *reinterpret_cast<uint4 *>(p) = pack<T>(x);
         else if constexpr (ACCESS == ANYWHERE) *reinterpret_cast<Unaligned *>(p) = __builtin_bit_cast(Unaligned, pack<T>(x));
@@ -57,19 +65,19 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T *table, int64_t 
         indices_at<LOOKUP_ROWS>(index, index_type, [&](int u) { return min(first + u * groups + group, n - 1); }, v);
         for (int32_t at = lane * P::W; at < width; at += lanes * P::W) {
             const int32_t c = P::column(at, width);
-            P p[LOOKUP_ROWS];
+            typename P::Stored stored[LOOKUP_ROWS];
             if (rows > 0) {                 // (loads from some row even where there is none to load: a load in a branch would wait for those before it)
 #pragma unroll
-                for (int u = 0; u < LOOKUP_ROWS; ++u) p[u].load(table + (v[u] >= 0 && v[u] < rows ? v[u] : 0) * ld_table + c);
+                for (int u = 0; u < LOOKUP_ROWS; ++u) stored[u] = P::fetch(table + (v[u] >= 0 && v[u] < rows ? v[u] : 0) * ld_table + c);
             }
 #pragma unroll
             for (int u = 0; u < LOOKUP_ROWS; ++u) {
-                p[u].scale(scale);
-                if (v[u] < 0 || v[u] >= rows) p[u].fill(v[u] == -1 ? 0.f : __builtin_nanf(""));
+                P p;
+                p.take(stored[u]);
+                p.scale(scale);
+                if (v[u] < 0 || v[u] >= rows) p.fill(v[u] == -1 ? 0.f : __builtin_nanf(""));
+                if (first + u * groups + group < n) p.store(out + (first + u * groups + group) * ld_out + c);
             }
-#pragma unroll
-            for (int u = 0; u < LOOKUP_ROWS; ++u)
-                if (first + u * groups + group < n) p[u].store(out + (first + u * groups + group) * ld_out + c);
         }
     }
 }
