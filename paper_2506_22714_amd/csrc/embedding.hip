@@ -52,7 +52,7 @@ template <class T, int ACCESS> struct Piece {
 };
 
 // ---- lookup ----
-// Four rows of each group of lanes in flight: 1,000,003 rows of 128 bytes in 39 us, 5 TB/s (one row of a wave at a time: 137 us).
+// Four rows of each group of lanes in flight, as they are in memory (as fp32 they take the registers of two waves): 1,000,003 rows of 128 bytes in 40 us, 5 TB/s (one row of a wave at a time: 137 us).
 constexpr int LOOKUP_ROWS = 4;
 
 template <class T, int ACCESS>
