@@ -838,6 +838,18 @@ def _ld(t) -> int:
     return t.shape[1] if t.is_contiguous() or t.shape[0] <= 1 else t.stride(0)
 
 
+def _apart(out, t, name: str):
+    """Refuses a result that lies on one of its inputs (columns of one array beside each other are fine)."""
+    a, b, size, ld = out.data_ptr(), t.data_ptr(), t.element_size(), _ld(t)
+    if out.numel() == 0 or t.numel() == 0:
+        return
+    if a >= b + ((t.shape[0] - 1) * ld + t.shape[1]) * size or b >= a + ((out.shape[0] - 1) * _ld(out) + out.shape[1]) * size:
+        return
+    column = (a - b) // size % ld
+    if _ld(out) != ld or column < t.shape[1] or column + out.shape[1] > ld:
+        raise ValueError(f"out: overlaps {name}")
+
+
 def _index_code(t, name: str, like) -> int:
     torch = _torch
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or not t.is_contiguous():
@@ -871,6 +883,7 @@ def embedding(table, index, scale: float = 1.0, out=None):
         _rows_of(out, "out", width, like=table)
         if out.shape[0] != n:
             raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+        _apart(out, table, "table")
         ld_out = _ld(out)
     _launch(lib().libra_embedding, "libra_embedding", table, table.data_ptr(), rows, width, _ld(table), dtype, index.data_ptr(), kind, n, scale,
             out.data_ptr(), ld_out)
@@ -895,6 +908,7 @@ def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
         _rows_of(out, "out", width, like=dout)
         if out.shape[0] != rows:
             raise ValueError(f"out: {out.shape[0]} rows, expected {rows}")
+        _apart(out, dout, "dout")
     ws = torch.empty(nb, dtype=torch.uint8, device=dout.device)
     _launch(lib().libra_embedding_backward, "libra_embedding_backward", dout, dout.data_ptr(), _ld(dout), dtype, index.data_ptr(), kind, n, rows,
             width, scale, out.data_ptr(), _ld(out), ws.data_ptr(), nb)
@@ -960,6 +974,7 @@ def log_probs_backward(logits, result: LogProbs, targets=None, d_target=None, d_
         _rows_of(out, "out", classes, like=logits)
         if out.shape[0] != n:
             raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+        _apart(out, logits, "logits")
     _launch(lib().libra_log_probs_backward, "libra_log_probs_backward", logits, logits.data_ptr(), n, classes, _ld(logits), dtype,
             targets.data_ptr() if targets is not None else 0, kind, top, scale, entropy, stats, result.top_index.data_ptr(), *grads,
             out.data_ptr(), _ld(out))

@@ -52,7 +52,8 @@ template <class T, int ACCESS> struct Piece {
 };
 
 // ---- lookup ----
-// Four rows of each group of lanes in flight, as they are in memory (as fp32 they take the registers of two waves): 1,000,003 rows of 128 bytes in 40 us, 5 TB/s (one row of a wave at a time: 137 us).
+// Four rows of each group of lanes in flight, as they are in memory (as fp32 they take the registers of two waves): 1,000,003 rows of 128 bytes
+// in 40 us, 5 TB/s (one row of a wave at a time: 137 us).
 constexpr int LOOKUP_ROWS = 4;
 
 template <class T, int ACCESS>
@@ -454,8 +455,9 @@ __global__ __launch_bounds__(PLACE_THREADS) void sort_place_kernel(Keys in, int6
     }
 }
 
-// Runs of `run` pairs, a group of lanes each, eight rows of dout in flight: 41 us for 2^20 rows of 128 bytes, 5 TB/s with what is written.  The row that a run begins in the middle of, and the one that goes on behind it, leave their
-// sums in `part` (two rows of fp32 for each run); a row that fills the whole run and goes on at both ends leaves the first of them.
+// Runs of `run` pairs, a group of lanes each, eight rows of dout in flight: 41 us for 2^20 rows of 128 bytes, 5 TB/s with what is written.
+// The row that a run begins in the middle of, and the one that goes on behind it, leave their sums in `part` (two rows of fp32 for each run);
+// a row that fills the whole run and goes on at both ends leaves the first of them.
 template <class T, int ACCESS>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *dout, int64_t ld_dout, const uint2 *pair, int64_t n, int32_t run, int64_t rows, int32_t width, float scale,
                                                        T *dtable, int64_t ld_dtable, float *part, int32_t part_width, int lanes) {

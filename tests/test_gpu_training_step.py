@@ -264,3 +264,22 @@ def test_the_optimizer_agrees_with_torch():
         b.step()
     for p, q in zip(ps, qs):
         assert float((p - q).detach().abs().max()) < 3 * 2.0 ** -24 * (40 * 1e-2 + 2 * 5)
+
+
+def test_results_on_their_inputs_are_refused():
+    """In place, shifted by a row or by a column; two halves of one array's columns are apart."""
+    held = torch.randn(40, 32, device="cuda")
+    x, t = held[:20, :16], torch.zeros(20, dtype=torch.int64, device="cuda")
+    r = lb.log_probs(x, t)
+    d = torch.ones(20, device="cuda")
+    index = torch.arange(20, device="cuda")
+    for out in (x, held[1:21, :16], held[:20, 8:24], held[:20, 15:31], held.reshape(80, 16)[:20]):
+        for call in (lambda: lb.log_probs_backward(x, r, t, d, out=out), lambda: lb.embedding(x, index, out=out),
+                     lambda: lb.embedding_backward(x, index, 20, out=out)):
+            with pytest.raises(ValueError, match="overlaps"):
+                call()
+    for out in (held[:20, 16:], held[20:, 3:19], held[5:25, 16:]):
+        before = x.clone()
+        assert torch.equal(lb.log_probs_backward(x, r, t, d, out=out), lb.log_probs_backward(before, r, t, d))
+        assert torch.equal(lb.embedding(x, index, 2.0, out=out), 2 * before) and torch.equal(lb.embedding_backward(x, index, 20, out=out), before)
+        assert torch.equal(x, before)
