@@ -377,7 +377,7 @@ struct Parts {                      // of rows that several workgroups share
     uint64_t *keys;                 // top for each
 };
 
-constexpr int LONG_THREADS = 256, ROUNDS = 8;
+constexpr int LONG_THREADS = 256, ROUNDS = 16;
 enum List { NONE, ONE_BY_ONE, SORTED };      // how the alternatives come
 
 // LDS of the waves of a row: what they exchange
@@ -394,10 +394,10 @@ template <int WAVES> __device__ inline void row_barrier() {
 template <int WAVES> __device__ inline int row_of_wave() { return WAVES * WAVE_LANES == LONG_THREADS ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / (WAVES * WAVE_LANES)); }
 
 // WAVES waves for a row or a part of it, 4 / WAVES rows for a workgroup.  A thread takes 16 logits a round.  The alternatives are looked for
-// after every eight rounds: each thread has kept the maximum of each of its rounds, and if every wave has `share` maxima that reach a rank, the
-// row has `top` logits that do, so that only the few rounds of a thread that reach it are read again, a lane each, and their logits go
-// through the list.
-// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 100 / 117 / 120 / 140 / 199.  When this way was chosen it took
+// after every sixteen rounds: each thread has kept the maximum of each of its rounds, and if every wave has `share` maxima that reach a rank,
+// the row has `top` logits that do, so that only the few rounds of a thread that reach it are read again, a lane each, and their logits go
+// through the list.  (After every eight rounds: 5,000 x 50,000 bf16 with 20 alternatives 137 us, not 123.)
+// 8,191 x 32,768 fp16, forward, in us with 0 / 1 / 5 / 20 / 64 alternatives: 100 / 110 / 118 / 138 / 188.  When this way was chosen it took
 // 94 / 122 / 123 / 145 / 216; looking at every logit as it comes by, with the same bound, 99 / 129 / 151 / 203 / 350, with each wave's own
 // list as the bound 97 / 129 / 191 / 364 / 757.  (Two rounds in flight instead of one: 5 to 14 % slower, fewer waves fit.)
 // A kernel of its own without alternatives has 60 registers, not 79 (16-bit logits): 20,000 classes 5.4 TB/s, not 5.0.  With them six waves on a
@@ -442,6 +442,7 @@ template <class T, int WAVES, List LIST> __global__ __launch_bounds__(LONG_THREA
         fetch(begin, raw);
         for (int32_t super = begin; super < end; super += ROUNDS * ROUND) {
             int rounds = 0;
+            float super_most = -INF;
             for (int32_t v0 = super; rounds < ROUNDS && v0 < end; v0 += ROUND, ++rounds) {
                 fetch(v0 + ROUND, next);                // on its way while this one is worked on
                 float y[N];
@@ -458,17 +459,15 @@ template <class T, int WAVES, List LIST> __global__ __launch_bounds__(LONG_THREA
 #pragma unroll
                 for (int k = 1; k < N; ++k) most = larger(most, y[k]);
                 a.template add<N>(y, most, c);
-                if constexpr (LIST != NONE) maxima[rounds][threadIdx.x] = most;
+                if constexpr (LIST != NONE) {
+                    maxima[rounds][threadIdx.x] = most;
+                    super_most = rounds ? larger(super_most, most) : most;
+                }
 #pragma unroll
                 for (int u = 0; u < U; ++u) raw[u] = next[u];
             }
             if constexpr (LIST == NONE) continue;
-            uint32_t rank[ROUNDS], largest = 0;
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) {
-                rank[r] = r < rounds ? rank_of(maxima[r][threadIdx.x]) : 0;
-                largest = max(largest, rank[r]);
-            }
+            const uint32_t largest = rank_of(super_most);
             floor = max(floor, wave_kth(largest, share));
             uint32_t least = floor;
             if constexpr (WAVES > 1) {
@@ -482,9 +481,8 @@ template <class T, int WAVES, List LIST> __global__ __launch_bounds__(LONG_THREA
             }
             least = max(least, (uint32_t)(best.limit >> 32));
             int many = 0;
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) {
-                const bool there = r < rounds && rank[r] >= least;
+            for (int r = 0; r < rounds; ++r) {
+                const bool there = rank_of(maxima[r][threadIdx.x]) >= least;
                 const uint64_t those = __ballot(there);
                 if (there) reaching[in_group][many + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(r * WAVE_LANES + lane);
                 many += (int)__popcll(those);
