@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "libra.h"
 
@@ -12,8 +13,13 @@ namespace libra {
 constexpr int WAVE_LANES = 64;
 
 template <class T> __device__ inline float load_as_float(T x) { return (float)x; }
-// one rounding to nearest even; NaN stays NaN, what is too large for the type becomes infinite
-template <class T> __device__ inline T round_to(float x) { return (T)x; }
+// One rounding of an fp32 number to nearest even; NaN stays NaN, what is too large for the type becomes infinite.  The compiler may not look
+// behind the number: it would merge a product or a sum with its rounding to fp16 into one instruction that rounds the exact value (not that to
+// bf16), and the last place of a result would go by how the code around it was compiled.
+template <class T> __device__ inline T round_to(float x) {
+    if constexpr (std::is_same_v<T, _Float16>) asm("" : "+v"(x));
+    return (T)x;
+}
 
 // 16 bytes of a row as numbers, and back
 template <class T> constexpr int VECTOR = 16 / (int)sizeof(T);

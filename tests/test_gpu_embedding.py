@@ -213,3 +213,19 @@ def test_refusals_of_the_binding():
             call()
     with pytest.raises(lb.LibraError):
         lb.libra_embedding_backward_workspace(3, -1, 8)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,width", [(5000, 6000, 128), (5000, 6000, 65), (5000, 6000, 3), (40000, 50000, 64), (40000, 50000, 67), (40000, 50000, 5)])
+def test_products_with_the_scale_are_formed_in_fp32(dtype, n, rows, width):
+    """A row of one id, or of two, is one fp32 product, rounded once more to its type: the same bits as the lookup's, in every way that the
+    gradient goes.  (0.7 times one fp16 number in forty is so near the middle of two that rounding the exact product gives another one.)"""
+    scale = float(np.float32(0.7))
+    g = torch.Generator(device="cuda").manual_seed(width)
+    whole = torch.randint(-2047, 2048, (n, width), generator=g, device="cuda").float() / 256           # sums of two are exact in fp32
+    dout = whole.to(dtype)
+    ids = torch.randperm(rows, generator=g, device="cuda")[:n]
+    ids[1::100] = ids[::100]
+    sums = torch.zeros(rows, width, device="cuda").index_add_(0, ids, dout.float())
+    assert torch.equal(lb.embedding_backward(dout, ids, rows, scale=scale), (sums * scale).to(dtype))
+    assert torch.equal(lb.embedding(dout, torch.arange(n, device="cuda"), scale=scale), (dout.float() * scale).to(dtype))

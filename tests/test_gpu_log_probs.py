@@ -397,3 +397,22 @@ def test_refusals_of_the_binding():
                  lambda: lb.log_probs(logits(2, 100, torch.float32), top=65)):
         with pytest.raises((lb.LibraError, RuntimeError)):
             call()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,classes", [(5000, 3), (5000, 40), (2000, 700), (2000, 2500), (64, 70000)])
+def test_products_with_the_scale_are_formed_in_fp32(dtype, n, classes):
+    """A masked class has no probability, so the gradient of its log probability is scale * d: an fp32 product, rounded once more."""
+    scale = float(np.float32(0.7))
+    x = torch.full((n, classes), -INF, device="cuda", dtype=dtype)
+    x[:, 1] = 0.0
+    t = torch.full((n,), classes - 1, dtype=torch.int64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(classes)
+    d = torch.randint(-2047, 2048, (n,), generator=g, device="cuda").float() / 256
+    got = lb.log_probs_backward(x, lb.log_probs(x, t, scale=scale), t, d, scale=scale)
+    assert torch.equal(got[:, classes - 1], (d * scale).to(dtype))
+    # and as one of the alternatives: the most likely class and the lowest masked one
+    r = lb.log_probs(x, t, top=2, scale=scale)
+    assert r.top_index[:, 1].tolist() == [0] * n
+    a = torch.stack([torch.zeros_like(d), d], 1)
+    assert torch.equal(lb.log_probs_backward(x, r, None, None, None, a, scale=scale)[:, 0], (d * scale).to(dtype))
