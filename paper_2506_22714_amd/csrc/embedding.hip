@@ -64,8 +64,8 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T *table, int64_t 
     for (int64_t first = (int64_t)blockIdx.x * (groups * LOOKUP_ROWS); first < n; first += (int64_t)gridDim.x * (groups * LOOKUP_ROWS)) {
         int64_t v[LOOKUP_ROWS];
         indices_at<LOOKUP_ROWS>(index, index_type, [&](int u) { return min(first + u * groups + group, n - 1); }, v);
-        for (int32_t at = lane * P::W; at < width; at += lanes * P::W) {
-            const int32_t c = P::column(at, width);
+        for (uint32_t at = lane * P::W; at < (uint32_t)width; at += lanes * P::W) {      // (unsigned: it passes the end of a row of up to 2^31 - 1)
+            const int32_t c = P::column((int32_t)at, width);
             typename P::Stored stored[LOOKUP_ROWS];
             if (rows > 0) {                 // (loads from some row even where there is none to load: a load in a branch would wait for those before it)
 #pragma unroll
@@ -621,7 +621,7 @@ struct Layout {                     // lanes of a row, rows of workgroups for wh
     unsigned slices;
 };
 Layout layout(int32_t width, int piece) {
-    const int32_t pieces = (width + piece - 1) / piece;
+    const int32_t pieces = width / piece + (width % piece != 0);
     int lanes = 1;
     while (lanes < WAVE_LANES && lanes < pieces) lanes *= 2;
     return {lanes, (unsigned)((pieces + lanes - 1) / lanes)};

@@ -229,3 +229,16 @@ def test_products_with_the_scale_are_formed_in_fp32(dtype, n, rows, width):
     sums = torch.zeros(rows, width, device="cuda").index_add_(0, ids, dout.float())
     assert torch.equal(lb.embedding_backward(dout, ids, rows, scale=scale), (sums * scale).to(dtype))
     assert torch.equal(lb.embedding(dout, torch.arange(n, device="cuda"), scale=scale), (dout.float() * scale).to(dtype))
+
+
+def test_the_widest_row():
+    """2^31 - 1 elements: columns are counted to beyond the end of a row."""
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("needs some 20 GiB")
+    table = torch.zeros(1, (1 << 31) - 1, dtype=torch.float16, device="cuda")
+    for at in (0, 1 << 30, (1 << 31) - 3000):
+        table[0, at:at + 3000].normal_()
+    got = lb.embedding(table, torch.tensor([0, -1], device="cuda"))
+    assert torch.equal(got[0], table[0]) and not bool(got[1].any())
+    del table, got
+    torch.cuda.empty_cache()
