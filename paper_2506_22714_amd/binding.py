@@ -834,6 +834,14 @@ def _rows_of(t, name: str, cols=None, like=None) -> int:
     return code
 
 
+def _width(t, name: str) -> int:
+    """Elements of a row, which the library counts in 32 bits."""
+    width = t.shape[1]
+    if not 1 <= width < 1 << 31:
+        raise ValueError(f"{name}: rows of {width or 'no'} elements")
+    return width
+
+
 def _ld(t) -> int:
     return t.shape[1] if t.is_contiguous() or t.shape[0] <= 1 else t.stride(0)
 
@@ -874,9 +882,7 @@ def embedding(table, index, scale: float = 1.0, out=None):
     torch = _gpu()
     dtype = _rows_of(table, "table")
     kind = _index_code(index, "index", table)
-    n, (rows, width) = index.numel(), table.shape
-    if width < 1:
-        raise ValueError("table: rows of no elements")
+    n, rows, width = index.numel(), table.shape[0], _width(table, "table")
     if out is None:
         out, ld_out = torch.empty(*index.shape, width, dtype=table.dtype, device=table.device), width
     else:
@@ -896,9 +902,7 @@ def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
     torch = _gpu()
     dtype = _rows_of(dout, "dout")
     kind = _index_code(index, "index", dout)
-    n, width = dout.shape
-    if width < 1:
-        raise ValueError("dout: rows of no elements")
+    n, width = dout.shape[0], _width(dout, "dout")
     if index.numel() != n:
         raise ValueError(f"index: {index.numel()} ids for {n} rows of dout")
     nb = libra_embedding_backward_workspace(n, rows, width)
@@ -935,6 +939,8 @@ def log_probs(logits, targets=None, top: int = 0, scale: float = 1.0) -> LogProb
         kind = _index_code(targets, "targets", logits)
         if targets.shape != (n,):
             raise ValueError(f"targets: shape {tuple(targets.shape)}, expected ({n},)")
+    if not 0 <= top <= classes:             # (here, too: it is passed on in 32 bits)
+        _check(ERR["SHAPE"], "libra_log_probs")
     nb = libra_log_probs_workspace(n, classes, top)
     device = logits.device
     target = torch.empty(n, dtype=torch.float32, device=device) if targets is not None else None

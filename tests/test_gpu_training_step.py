@@ -283,3 +283,18 @@ def test_results_on_their_inputs_are_refused():
         assert torch.equal(lb.log_probs_backward(x, r, t, d, out=out), lb.log_probs_backward(before, r, t, d))
         assert torch.equal(lb.embedding(x, index, 2.0, out=out), 2 * before) and torch.equal(lb.embedding_backward(x, index, 20, out=out), before)
         assert torch.equal(x, before)
+
+
+def test_numbers_that_32_bits_do_not_hold():
+    """Refused, not cut to 32 bits.  (Tensors without rows: they take no memory.)"""
+    none = torch.zeros(0, dtype=torch.int64, device="cuda")
+    for width in (1 << 31, (1 << 32) + 8):
+        x = torch.empty(0, width, device="cuda")
+        with pytest.raises(ValueError, match="elements"):
+            lb.embedding(x, none)
+        with pytest.raises(ValueError, match="elements"):
+            lb.embedding_backward(x, none, 0)
+    for top in ((1 << 32) + 1, (1 << 33) + 2, 3 - (1 << 32)):
+        for n in (0, 2):
+            with pytest.raises(RuntimeError):
+                lb.log_probs(torch.zeros(n, 10, device="cuda"), top=top)

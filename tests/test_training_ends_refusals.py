@@ -142,3 +142,11 @@ def test_the_optimizer_refuses():
     for kw in (dict(state_bits=16), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1.0), dict(lr=torch.tensor(1e-3))):
         with pytest.raises(ValueError):
             AdamW(p, **kw)
+
+
+def test_widths_that_32_bits_do_not_hold():
+    """(Tensors without rows: they take no memory.)"""
+    for width in (0, 1 << 31, (1 << 32) + 8):
+        with pytest.raises(ValueError, match="elements"):
+            lb._width(torch.empty(0, width), "table")
+    assert lb._width(torch.empty(0, (1 << 31) - 1), "table") == (1 << 31) - 1
