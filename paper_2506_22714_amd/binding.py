@@ -1004,6 +1004,15 @@ def _one_on(x, name: str, dtype, like) -> int:
     return x.data_ptr()
 
 
+class _AdamwCall(NamedTuple):
+    """A step whose tensors have been looked at: what the library takes, and the tensors, which have to live until it has run."""
+    table: bytes
+    count: int
+    opts: AdamwOpts
+    params: object
+    held: object
+
+
 def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
           first_scales=None, second_scales=None, masters=None, seed: int = 0, numbers=None):
     """One AdamW step, in place, over lists of contiguous tensors on one GPU.
@@ -1013,6 +1022,18 @@ def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: 
     which the 16-bit ones are the roundings (a list, None where a tensor has none).  ``step`` counts from 1.  ``step`` and ``lr`` may be
     one-element tensors on the GPU (int64, float32): they are read when the kernel runs, also of a captured step.  ``seed``, ``numbers``
     (of the tensors; their places in the list): of the chances by which 8-bit states are rounded."""
+    call = _adamw_checked(params, grads, first, second, step, lr, betas, eps, weight_decay, first_scales, second_scales, masters, seed, numbers)
+    if call is not None:
+        _adamw_run(call)
+
+
+def _adamw_run(call: _AdamwCall):
+    _launch(lib().libra_adamw, "libra_adamw", call.params[0], call.table, call.count, C.byref(call.opts))
+    _torch.autograd.graph.increment_version(call.params)           # a graph that saved one of them must notice
+
+
+def _adamw_checked(params, grads, first, second, step, lr, betas, eps, weight_decay, first_scales, second_scales, masters, seed, numbers):
+    """The call of :func:`adamw` with these arguments; None if there is nothing to do."""
     torch = _gpu()
     count = len(params)
     bits8 = first_scales is not None
@@ -1023,7 +1044,7 @@ def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: 
         if x is not None and len(x) != count:
             raise ValueError(f"{name}: {len(x)} tensors for {count} parameters")
     if count == 0:
-        return
+        return None
     state = torch.float8_e4m3fn if bits8 else torch.float32
     device = params[0].get_device()
     if device < 0:
@@ -1071,5 +1092,4 @@ def adamw(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps: 
         opts.lr_dev = _one_on(lr, "lr", torch.float32, params[0])
     else:
         opts.lr = lr
-    _launch(lib().libra_adamw, "libra_adamw", params[0], table, count, C.byref(opts))
-    torch.autograd.graph.increment_version(params)           # a graph that saved one of them must notice
+    return _AdamwCall(table, count, opts, params, (grads, first, second, first_scales, second_scales, masters, step, lr))

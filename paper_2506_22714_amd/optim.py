@@ -51,29 +51,44 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        number = 0
-        for group in self.param_groups:
-            # parameters whose gradients came and went may stand at different steps: one call for each of them.  The tensor's number, by
-            # which 8-bit states draw their chances, is its place among all parameters, whoever has a gradient
-            calls = {}
-            if group["capturable"]:
-                if "step" not in group:
+        number, runs, new = 0, [], []
+        try:
+            for group in self.param_groups:
+                # parameters whose gradients came and went may stand at different steps: one call for each of them.  The tensor's number, by
+                # which 8-bit states draw their chances, is its place among all parameters, whoever has a gradient
+                calls = {}
+                if group["capturable"] and "step" not in group:
                     self._not_captured()
                     group["step"] = torch.zeros((), dtype=torch.int64, device=group["params"][0].device)
-                group["step"] += 1
-            for p in group["params"]:
-                number += 1
-                if p.grad is None:
-                    continue
-                if p not in self.state or not self.state[p]:
-                    self._not_captured()
-                    self.state[p] = self._new_state(p, group)
-                s = self.state[p]
-                if not group["capturable"]:
-                    s["step"] += 1
-                calls.setdefault((p.get_device(), s.get("step")), []).append((number - 1, p, s))
-            for (_, step), members in calls.items():
-                self._call(group, members, group["step"] if step is None else step)
+                for p in group["params"]:
+                    number += 1
+                    if p.grad is None:
+                        continue
+                    if p not in self.state or not self.state[p]:
+                        self._not_captured()
+                        self.state[p] = self._new_state(p, group)
+                        new.append(p)
+                    s = self.state[p]
+                    calls.setdefault((p.get_device(), s.get("step")), []).append((number - 1, p, s))
+                runs.append((group, [(members, self._checked(group, members, group["step"] if step is None else step + 1))
+                                     for (_, step), members in calls.items()]))
+        except Exception:               # nothing has been counted or changed
+            for p in new:
+                del self.state[p]
+            raise
+        for group, calls in runs:
+            if group["capturable"]:
+                group["step"] += 1      # before the kernel reads it
+            try:
+                for members, call in calls:
+                    lb._adamw_run(call)
+                    for _, _, s in members:
+                        if "step" in s:
+                            s["step"] += 1
+            except Exception:
+                if group["capturable"]:
+                    group["step"] -= 1
+                raise
         return loss
 
     def load_state_dict(self, state_dict):
@@ -88,12 +103,14 @@ class AdamW(torch.optim.Optimizer):
             if isinstance(g.get("step"), torch.Tensor):
                 g["step"] = g["step"].to(g["params"][0].device)
 
-    def _call(self, group, members, step):
+    def _checked(self, group, members, step):
+        """The call, looked at: its tensors here, its options by a call without tensors."""
         bits8 = group["state_bits"] == 8
         params = [p for _, p, _ in members]
         states = [s for _, _, s in members]
-        lb.adamw(params, [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params], [s["first"] for s in states],
-                 [s["second"] for s in states], step, lr=group["lr"], betas=group["betas"], eps=group["eps"],
-                 weight_decay=group["weight_decay"], first_scales=[s["first_scales"] for s in states] if bits8 else None,
-                 second_scales=[s["second_scales"] for s in states] if bits8 else None,
-                 masters=[s.get("master") for s in states] if group["master"] else None, seed=group["seed"], numbers=[k for k, _, _ in members])
+        call = lb._adamw_checked(params, [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params], [s["first"] for s in states],
+                                 [s["second"] for s in states], step, group["lr"], group["betas"], group["eps"], group["weight_decay"],
+                                 [s["first_scales"] for s in states] if bits8 else None, [s["second_scales"] for s in states] if bits8 else None,
+                                 [s.get("master") for s in states] if group["master"] else None, group["seed"], [k for k, _, _ in members])
+        lb.libra_adamw(None, 0, call.opts)
+        return call

@@ -423,3 +423,43 @@ def test_optimizer_under_capture():
         for x, y in zip(a, b):
             assert torch.equal(oa.state[x]["first"].view(torch.uint8), ob.state[y]["first"].view(torch.uint8))
             assert float((x - y).abs().max()) < 1e-6
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_refused_step_counts_for_nothing(bits, capturable):
+    """Whatever is refused, in whichever group: no parameter, state or count has changed, and the steps after it are what they would have been."""
+    from paper_2506_22714_amd.optim import AdamW
+    def make():
+        ps = [torch.nn.Parameter(torch.linspace(-1, 1, n, device="cuda")) for n in (300, 7, 40)]
+        return ps, AdamW([{"params": ps[:2]}, {"params": ps[2:], "lr": 1e-2}], lr=1e-3, state_bits=bits, capturable=capturable, seed=3)
+    (ps, opt), (qs, plain) = make(), make()
+    odd = torch.nn.Parameter(torch.ones(4, device="cuda", dtype=torch.float64))          # no type of the kernels
+    opt.add_param_group({"params": [odd]})
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for step in range(3):
+        for p, q in zip(ps, qs):
+            p.grad = torch.randn(p.shape, generator=g, device="cuda")
+            q.grad = p.grad.clone()
+        before = [p.detach().clone() for p in ps]
+        odd.grad = torch.ones_like(odd)
+        with pytest.raises(ValueError):
+            opt.step()
+        odd.grad = None
+        for name, bad in (("lr", float("nan")), ("eps", float("nan")), ("betas", (0.9, 1.0))):
+            good, opt.param_groups[1][name] = opt.param_groups[1][name], bad
+            with pytest.raises(lb.LibraError):
+                opt.step()
+            opt.param_groups[1][name] = good
+        assert all(torch.equal(p, b) for p, b in zip(ps, before))
+        assert len(opt.state) == (3 if step else 0)
+        opt.step()
+        plain.step()
+        for p, q in zip(ps, qs):
+            assert torch.equal(p, q)
+            a, b = opt.state[p], plain.state[q]
+            assert a.get("step") == b.get("step") == (None if capturable else step + 1)
+            for name in ("first", "second"):
+                assert torch.equal(a[name].view(torch.uint8), b[name].view(torch.uint8))
+        if capturable:
+            assert [int(group["step"]) for group in opt.param_groups[:2]] == [step + 1] * 2
