@@ -13,7 +13,8 @@ class AdamW(torch.optim.Optimizer):
     ``master``: 16-bit parameters are the roundings of copies in 32 bits that are kept with the states; without it every step rounds the
     parameter itself, and steps below half of its last place are lost.
     ``capturable``: the step number is kept on the GPU, so that a captured step counts on, one number for a group (a parameter without a
-    gradient skips the step, the number does not); ``lr`` may then be a one-element float32 tensor there, too.  Parameters are contiguous tensors of float16, bfloat16 or float32 on one GPU; gradients are of the same type."""
+    gradient skips the step, the number does not); ``lr`` may then be a one-element float32 tensor there, too.  Other steps are not captured.
+    Parameters are contiguous tensors of float16, bfloat16 or float32 on one GPU; gradients are of the same type."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, state_bits: int = 32,
                  master: bool = False, capturable: bool = False, seed: int = 0):
@@ -70,6 +71,8 @@ class AdamW(torch.optim.Optimizer):
                         new.append(p)
                     s = self.state[p]
                     calls.setdefault((p.get_device(), s.get("step")), []).append((number - 1, p, s))
+                if calls and not group["capturable"] and torch.cuda.is_current_stream_capturing():      # every replay would repeat one step number
+                    raise RuntimeError("a captured step needs capturable=True")
                 runs.append((group, [(members, self._checked(group, members, group["step"] if step is None else step + 1))
                                      for (_, step), members in calls.items()]))
         except Exception:               # nothing has been counted or changed

@@ -463,3 +463,23 @@ def test_a_refused_step_counts_for_nothing(bits, capturable):
                 assert torch.equal(a[name].view(torch.uint8), b[name].view(torch.uint8))
         if capturable:
             assert [int(group["step"]) for group in opt.param_groups[:2]] == [step + 1] * 2
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_that_counts_on_the_host_is_not_captured(bits):
+    """Its number would be the same in every replay."""
+    from paper_2506_22714_amd.optim import AdamW
+    p, q = (torch.nn.Parameter(torch.ones(300, device="cuda")) for _ in range(2))
+    p.grad, q.grad = torch.ones_like(p), torch.ones_like(q)
+    opt = AdamW([{"params": [q], "capturable": True}, {"params": [p]}], state_bits=bits)
+    opt.step()
+    before = p.detach().clone(), q.detach().clone()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="capturable"):
+        with torch.cuda.graph(graph):
+            opt.step()
+    torch.cuda.synchronize()
+    assert opt.state[p]["step"] == 1 and int(opt.param_groups[0]["step"]) == 1
+    assert torch.equal(p, before[0]) and torch.equal(q, before[1])
+    opt.step()
+    assert opt.state[p]["step"] == 2
