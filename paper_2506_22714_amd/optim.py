@@ -94,7 +94,11 @@ class AdamW(torch.optim.Optimizer):
                 raise
         return loss
 
+    @torch.no_grad()
     def load_state_dict(self, state_dict):
+        """The numbers of a checkpoint, wherever it was loaded to.  A rate that is a tensor stays the one that the program fills; a captured
+        step has to be captured again (states are new tensors)."""
+        rates = [g["lr"] for g in self.param_groups]
         super().load_state_dict(state_dict)
         # the base class converts states to their parameters' types: these keep their own
         saved = [k for g in state_dict["param_groups"] for k in g["params"]]
@@ -102,9 +106,16 @@ class AdamW(torch.optim.Optimizer):
             for name, x in state_dict["state"].get(k, {}).items():
                 if isinstance(x, torch.Tensor):
                     self.state[p][name] = x.detach().to(p.device, copy=True)
-        for g in self.param_groups:
+        filled = {}                     # groups may share a rate, as long as what is loaded is the same
+        for g, rate in zip(self.param_groups, rates):
+            device = g["params"][0].device
             if isinstance(g.get("step"), torch.Tensor):
-                g["step"] = g["step"].to(g["params"][0].device)
+                g["step"] = g["step"].to(device)
+            if isinstance(g["lr"], torch.Tensor):
+                if isinstance(rate, torch.Tensor) and float(filled.setdefault(id(rate), g["lr"])) == float(g["lr"]):
+                    g["lr"] = rate.copy_(g["lr"].reshape(rate.shape))
+                else:
+                    g["lr"] = g["lr"].to(device)
 
     def _checked(self, group, members, step):
         """The call, looked at: its tensors here, its options by a call without tensors."""

@@ -483,3 +483,62 @@ def test_a_step_that_counts_on_the_host_is_not_captured(bits):
     assert torch.equal(p, before[0]) and torch.equal(q, before[1])
     opt.step()
     assert opt.state[p]["step"] == 2
+
+
+@pytest.mark.parametrize("handle", [True, False])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_checkpoint_on_the_cpu_goes_on(bits, handle):
+    """Step numbers and rates on the GPU, saved, loaded to the CPU and from there into another optimizer: its steps are those of the first one.
+    A rate that the program holds is filled, and read."""
+    import io
+    from paper_2506_22714_amd.optim import AdamW
+    def make(lr):
+        ps = [torch.nn.Parameter(torch.linspace(-1, 1, n, device="cuda").bfloat16()) for n in (300, 7)]
+        return ps, AdamW([{"params": ps[:1]}, {"params": ps[1:], "lr": 5e-3}], lr=lr, state_bits=bits, master=True, capturable=True, seed=2)
+    lr = torch.full((1,), 1e-2, device="cuda")
+    ps, opt = make(lr)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    def grads(*several):
+        for k, n in enumerate((300, 7)):
+            d = torch.randn(n, generator=g, device="cuda").bfloat16()
+            for s in several:
+                s[k].grad = d.clone()
+    for _ in range(2):
+        grads(ps)
+        opt.step()
+    file = io.BytesIO()
+    torch.save(opt.state_dict(), file)
+    file.seek(0)
+    other = torch.zeros((), device="cuda") if handle else 0.5
+    qs, again = make(other)
+    again.load_state_dict(torch.load(file, map_location="cpu", weights_only=True))
+    for p, q in zip(ps, qs):
+        q.data.copy_(p.data)
+    if handle:
+        assert again.param_groups[0]["lr"] is other and float(other) == float(lr)
+    assert again.param_groups[0]["lr"].device == ps[0].device and again.param_groups[1]["lr"] == 5e-3
+    for k in range(3):
+        if k == 1:
+            lr.fill_(3e-2)
+            again.param_groups[0]["lr"].fill_(3e-2)
+        grads(ps, qs)
+        opt.step()
+        again.step()
+        assert [int(x["step"]) for x in again.param_groups] == [k + 3] * 2
+        for p, q in zip(ps, qs):
+            assert torch.equal(p, q)
+            for name, x in opt.state[p].items():
+                assert torch.equal(x.view(torch.uint8), again.state[q][name].view(torch.uint8))
+
+
+def test_rates_that_groups_share():
+    """Two groups with one tensor take rates that differ apart."""
+    from paper_2506_22714_amd.optim import AdamW
+    make = lambda a, b: AdamW([{"params": [torch.nn.Parameter(torch.ones(3, device="cuda"))], "lr": x} for x in (a, b)], capturable=True)      # noqa: E731
+    rate = lambda x: torch.full((1,), x, device="cuda")       # noqa: E731
+    for want in ((1e-2, 1e-2), (1e-2, 2e-2)):
+        shared = rate(5.0)
+        opt = make(shared, shared)
+        opt.load_state_dict(make(rate(want[0]), rate(want[1])).state_dict())
+        assert [float(g["lr"]) for g in opt.param_groups] == [float(torch.tensor(x)) for x in want]
+        assert opt.param_groups[0]["lr"] is shared and (opt.param_groups[1]["lr"] is shared) == (want[0] == want[1])
