@@ -434,11 +434,12 @@ int libra_log_probs_backward(const void *logits, int64_t n, int64_t classes, int
  * word of i) + (high word of i) * 0x9E3779B1), key = mix(mix(mix(seed) + t) + number), all modulo 2^32; (h mod 2^16) / 2^16 for m, (h div
  * 2^16) / 2^16 for the root; mix(x): x ^= x >> 16, x *= 0x6C8E9CF5, x ^= x >> 15, x *= 0x58AC4D6B, x ^= x >> 16.  The same step gives
  * the same bits every time.
- *   tensors    host, read during the call.  Their arrays are on the device, n elements each without gaps, and do not overlap
+ *   tensors    host, read during the call.  Their arrays are on the device, n elements each without gaps; what is written does not overlap
+ *              anything else (gradients may lie on each other, and `master` may be `param` where that is fp32)
  *   opts       host.  step_dev, lr_dev: device, or NULL: then t and lr are read when the kernel runs, instead of `step` and `lr` (a
  *              captured step counts on and follows a schedule)
- * Errors: NULL, SHAPE, TOO_LARGE, DTYPE, OPTION, BUFFER (an array not aligned to its elements), HIP.  Nothing is changed by a call that
- * is refused for its arguments.
+ * Errors: NULL, SHAPE, TOO_LARGE, DTYPE, OPTION, BUFFER (an array not aligned to its elements, or on another one), NOMEM, HIP.  Nothing is
+ * changed by a call that is refused for its arguments.
  */
 #define LIBRA_ADAMW_BLOCK 256
 typedef struct {

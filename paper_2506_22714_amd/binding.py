@@ -1051,7 +1051,7 @@ def _adamw_checked(params, grads, first, second, step, lr, betas, eps, weight_de
         raise ValueError("params[0]: must be a GPU tensor")
     float32 = torch.float32
     codes = {torch.float16: F16, torch.bfloat16: BF16, float32: F32}
-    fields, seen = [], set()            # a record of AdamwTensor is eight words and two halves of one
+    fields = []                         # a record of AdamwTensor is eight words and two halves of one
     for k, p in enumerate(params):
         g, m, v = grads[k], first[k], second[k]
         ms, vs = (first_scales[k], second_scales[k]) if bits8 else (None, None)
@@ -1074,14 +1074,15 @@ def _adamw_checked(params, grads, first, second, step, lr, betas, eps, weight_de
             more = [("first_scales", ms, float32, -(-n // ADAMW_BLOCK)), ("second_scales", vs, float32, -(-n // ADAMW_BLOCK))] if bits8 else []
             _adamw_refuse(k, [("params", p, p.dtype, n), ("grads", g, p.dtype, n), ("first", m, state, n), ("second", v, state, n), *more,
                               *([("masters", w, float32, n)] if w is not None else [])], p.dtype, n, device)
-        at = p.data_ptr()
-        if n:
-            if at in seen:
-                raise ValueError(f"params[{k}]: the same tensor twice")
-            seen.add(at)
         number = k if numbers is None else numbers[k] & 0xffffffff
-        fields += (at, g.data_ptr(), m.data_ptr(), v.data_ptr(), ms.data_ptr() if bits8 else 0, vs.data_ptr() if bits8 else 0,
+        fields += (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms.data_ptr() if bits8 else 0, vs.data_ptr() if bits8 else 0,
                    w.data_ptr() if w is not None else 0, n, codes[dtype] | number << 32)
+    if len(set(fields[::9])) < count:
+        seen = set()
+        for k, p in enumerate(params):
+            if p.numel() and p.data_ptr() in seen:
+                raise ValueError(f"params[{k}]: the same tensor twice")
+            seen.add(p.data_ptr())
     table = struct.pack(f"{len(fields)}Q", *fields)
     opts = AdamwOpts(state_bits=8 if bits8 else 32, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=seed & 0xffffffff)
     if isinstance(step, torch.Tensor):

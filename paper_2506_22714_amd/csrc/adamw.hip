@@ -13,6 +13,8 @@
 // by the vector ALUs: 167 us, 4.0 TB/s.
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "ends.h"
 
@@ -283,6 +285,43 @@ int check(const libra_adamw_tensor_t &t, bool bits8) {
     return LIBRA_OK;
 }
 
+// Every array that is written lies apart from all others.  (Gradients may lie on each other, and a copy on its parameter where that is fp32:
+// both get the same numbers from the same threads.)  19 tensors: 1 us.
+struct Place {
+    uintptr_t begin, end;
+    bool written;
+};
+int check_places(const libra_adamw_tensor_t *tensors, int32_t count, bool bits8) {
+    Place few[LAUNCH_TENSORS * 7];
+    std::unique_ptr<Place[]> many;
+    Place *place = few;
+    if (count > LAUNCH_TENSORS) {
+        many.reset(new (std::nothrow) Place[(size_t)count * 7]);
+        if (!(place = many.get())) return LIBRA_ERR_NOMEM;
+    }
+    size_t places = 0;
+    auto add = [&](const void *p, size_t bytes, bool written) { place[places++] = {(uintptr_t)p, (uintptr_t)p + bytes, written}; };
+    for (int32_t k = 0; k < count; ++k) {
+        const libra_adamw_tensor_t &t = tensors[k];
+        if (t.n == 0) continue;
+        const size_t n = (size_t)t.n, scales = (n + STATE_BLOCK - 1) / STATE_BLOCK * 4, state = bits8 ? 1 : 4;
+        add(t.param, n * dtype_bytes(t.dtype), true);
+        add(t.grad, n * dtype_bytes(t.dtype), false);
+        add(t.first, n * state, true);
+        add(t.second, n * state, true);
+        if (bits8) add(t.first_scales, scales, true), add(t.second_scales, scales, true);
+        if (t.master && !(t.dtype == LIBRA_F32 && t.master == t.param)) add(t.master, n * 4, true);
+    }
+    std::sort(place, place + places, [](const Place &a, const Place &b) { return a.begin < b.begin; });
+    uintptr_t end = 0, written_end = 0;         // of what begins before
+    for (size_t k = 0; k < places; ++k) {
+        if (place[k].begin < (place[k].written ? end : written_end)) return LIBRA_ERR_BUFFER;
+        end = std::max(end, place[k].end);
+        if (place[k].written) written_end = std::max(written_end, place[k].end);
+    }
+    return LIBRA_OK;
+}
+
 }  // namespace
 
 extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, const libra_adamw_opts_t *o, void *stream) {
@@ -296,6 +335,7 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
     const bool bits8 = o->state_bits == 8;
     for (int32_t k = 0; k < count; ++k)
         if (int rc = check(tensors[k], bits8)) return rc;
+    if (int rc = check_places(tensors, count, bits8)) return rc;
     Step s{};
     s.b1 = (float)o->beta1;
     s.b2 = (float)o->beta2;

@@ -542,3 +542,38 @@ def test_rates_that_groups_share():
         opt.load_state_dict(make(rate(want[0]), rate(want[1])).state_dict())
         assert [float(g["lr"]) for g in opt.param_groups] == [float(torch.tensor(x)) for x in want]
         assert opt.param_groups[0]["lr"] is shared and (opt.param_groups[1]["lr"] is shared) == (want[0] == want[1])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_arrays_beside_each_other_and_shared_gradients(bits):
+    """Parameters and states cut from one array each, without space between; a gradient that two parameters have; an fp32 copy that is its
+    parameter.  What is written may not lie on anything else."""
+    n = [256, 300, 20, 5000]
+    at = np.concatenate([[0], np.cumsum(n)])
+    def make(apart):
+        cut = lambda t: [t[a:b].clone() if apart else t[a:b] for a, b in zip(at, at[1:])]      # noqa: E731
+        f = lambda seed: torch.randn(int(at[-1]), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")      # noqa: E731
+        p = cut(f(0))
+        g = f(1)
+        grads = [g[:k] for k in n]                # all begin at one address
+        if bits == 8:
+            states = [[x.to(torch.float8_e4m3fn) for x in cut(f(2))], [x.to(torch.float8_e4m3fn) for x in cut(f(3).abs())]]
+            return p, grads, *states, *[[torch.ones(-(-k // 256), device="cuda") for k in n] for _ in range(2)]
+        return p, grads, cut(f(2)), cut(f(3).abs()), None, None
+    runs = []
+    for apart in (False, True):
+        p, g, m, v, ms, vs = make(apart)
+        masters = None if apart else [p[0], None, p[2], None]
+        lb.adamw(p, g, m, v, 3, **HYPER, first_scales=ms, second_scales=vs, masters=masters)
+        runs.append([*p, *m, *v, *(ms or []), *(vs or [])])
+    for a, b in zip(*runs):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    p, g, m, v, ms, vs = make(False)
+    before = [t.clone() for t in (*p, *m, *v)]
+    held = torch.zeros(6000, device="cuda")
+    for bad in (dict(params=[held[:256], held[255:555], *p[2:]]), dict(grads=[p[0], *g[1:]]), dict(grads=[p[3][1:257], *g[1:]]), dict(first=v),
+                dict(params=[*p[:3], held[:5000]], masters=[None, None, None, held[1000:]])):
+        with pytest.raises(lb.LibraError):
+            lb.adamw(**{**dict(params=p, grads=g, first=m, second=v, step=3, first_scales=ms, second_scales=vs), **bad})
+    for t, b in zip((*p, *m, *v), before):
+        assert torch.equal(t.view(torch.uint8), b.view(torch.uint8))

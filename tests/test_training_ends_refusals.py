@@ -150,3 +150,26 @@ def test_widths_that_32_bits_do_not_hold():
         with pytest.raises(ValueError, match="elements"):
             lb._width(torch.empty(0, width), "table")
     assert lb._width(torch.empty(0, (1 << 31) - 1), "table") == (1 << 31) - 1
+
+
+def test_adamw_refuses_arrays_that_overlap():
+    """Addresses that nothing is read from: the call is refused before."""
+    def call(bits, dtype=lb.F32, n=300, tensors=2, **places):
+        table = (lb.AdamwTensor * tensors)()
+        for k in range(tensors):
+            at = dict(zip(("param", "grad", "first", "second", "first_scales", "second_scales", "master"), range((1 + 7 * k) << 20, (8 + 7 * k) << 20, 1 << 20)))
+            table[k] = lb.AdamwTensor(**at, n=n, dtype=dtype)
+        for name, value in places.items():
+            setattr(table[tensors - 1], name, value)
+        return adamw(bits, tensors=table, count=tensors)
+    size = {"param": 1200, "first": 1200, "second": 1200, "master": 1200, "first_scales": 8, "second_scales": 8, "grad": 1200}
+    first = {name: (k + 1) << 20 for k, name in enumerate(("param", "grad", "first", "second", "first_scales", "second_scales", "master"))}
+    for bits in (32, 8):
+        for tensors in (2, 40):
+            for name in size:
+                for other, begin in first.items():
+                    if bits == 32 and "scales" in name + other or name == other == "grad":
+                        continue
+                    bytes_of = lambda x: 300 if bits == 8 and x in ("first", "second") else size[x]       # noqa: E731
+                    for at in (begin, begin + bytes_of(other) - 4, begin - bytes_of(name) + 4):
+                        assert call(bits, tensors=tensors, **{name: at}) == E["BUFFER"], (bits, tensors, name, other)
