@@ -853,9 +853,13 @@ def _apart(out, t, name: str):
         return
     if a >= b + ((t.shape[0] - 1) * ld + t.shape[1]) * size or b >= a + ((out.shape[0] - 1) * _ld(out) + out.shape[1]) * size:
         return
-    column = (a - b) // size % ld
-    if _ld(out) != ld or column < t.shape[1] or column + out.shape[1] > ld:
-        raise ValueError(f"out: overlaps {name}")
+    lds = {_ld(x) for x in (out, t) if x.shape[0] > 1}       # (one row goes by the distance of the other's rows)
+    if len(lds) == 1:
+        (ld,) = lds
+        column = (a - b) // size % ld
+        if column >= t.shape[1] and column + out.shape[1] <= ld:
+            return
+    raise ValueError(f"out: overlaps {name}")
 
 
 def _index_code(t, name: str, like) -> int:

@@ -173,3 +173,26 @@ def test_adamw_refuses_arrays_that_overlap():
                     bytes_of = lambda x: 300 if bits == 8 and x in ("first", "second") else size[x]       # noqa: E731
                     for at in (begin, begin + bytes_of(other) - 4, begin - bytes_of(name) + 4):
                         assert call(bits, tensors=tensors, **{name: at}) == E["BUFFER"], (bits, tensors, name, other)
+
+
+def test_a_row_beside_the_columns_that_are_written():
+    """By places: a result lies on its input or not, whichever of them has a single row."""
+    held = torch.zeros(12, 16)
+    places = torch.arange(12 * 16).view(12, 16)
+    def cut(x, rows, cols):
+        return x[slice(*rows), slice(*cols)]
+    some = [((a, b), (c, d)) for a, b in ((0, 12), (0, 1), (5, 6), (11, 12), (3, 7)) for c, d in ((0, 16), (0, 8), (8, 16), (3, 9), (8, 12), (15, 16))]
+    apart = 0
+    for one in some:
+        for two in some:
+            out, t = cut(held, *one), cut(held, *two)
+            lie_on = bool(torch.isin(cut(places, *one).contiguous(), cut(places, *two).contiguous()).any())
+            if lie_on:
+                with pytest.raises(ValueError, match="overlaps"):
+                    lb._apart(out, t, "t")
+            else:
+                lb._apart(out, t, "t")
+                apart += 1
+    assert apart > 300
+    with pytest.raises(ValueError, match="overlaps"):
+        lb._apart(held.view(24, 8)[1:3], held[:, :8], "t")          # rows of other distances: not looked at any further
