@@ -395,7 +395,7 @@ int libra_embedding_backward(const void *dout, int64_t ld_dout, int dtype, const
  * class first).  All sums in fp32.
  *   logits     device, n x classes with row stride ld elements, values of `dtype`;  n, classes < 2^31
  *   targets    device, n classes (index_type), or NULL.  -1: none, log probability 0; another number outside [0, classes): NaN
- *   top        0 .. LIBRA_LOG_PROBS_MAX_TOP and not above `classes`;  scale  finite, above 0
+ *   top        0 .. LIBRA_LOG_PROBS_MAX_TOP and not above `classes`;  scale  above 0, 2^127 at most
  *   target_out, entropy  device, fp32[n];  top_out  fp32[n * top], top_index  int64[n * top] (NULL where targets or top are)
  *   stats      device, fp32[2 n]: the largest logit and log sum exp(scale * (x - largest)) of each row, for the backward call
  *   workspace  device, 256-byte aligned, libra_log_probs_workspace() bytes (0: may be NULL), not needed after the call has run

@@ -7,7 +7,6 @@
 // The forward pass reads the logits once: maximum, s and sum exp(z) z run along and are rescaled where the maximum grows, and the best
 // logits are kept in the lanes of a wave.  The backward pass reads them once more and writes as much.  Both are bound by memory.
 #include <algorithm>
-#include <cmath>
 
 #include "ends.h"
 
@@ -745,6 +744,9 @@ int32_t part_count(int64_t n, int64_t classes) {
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(wanted, most), MAX_PARTS));
 }
 
+// (times log2 e a larger one is infinite)
+bool known_scale(float scale) { return scale > 0.f && scale <= 0x1p127f; }
+
 size_t part_bytes(int64_t n, int32_t count, int32_t top) { return count == 1 ? 0 : ((size_t)n * count * 12 + 255) / 256 * 256 + (size_t)n * count * top * 8; }
 
 // f(lanes of a row, numbers of a lane) for rows that with their neighbours' numbers in the first piece have `numbers`; a lane has EACH or
@@ -786,7 +788,7 @@ extern "C" int libra_log_probs(const void *logits, int64_t n, int64_t classes, i
     if (int rc = shape(n, classes, top)) return rc;
     if (ld < classes) return LIBRA_ERR_SHAPE;
     if (!known_dtype(dtype)) return LIBRA_ERR_DTYPE;
-    if ((targets && !known_index(index_type)) || !(scale > 0.f && std::isfinite(scale))) return LIBRA_ERR_OPTION;
+    if ((targets && !known_index(index_type)) || !known_scale(scale)) return LIBRA_ERR_OPTION;
     if (n == 0) return LIBRA_OK;
     if (!logits || !entropy || !stats || (targets && !target_out) || (top && (!top_out || !top_index))) return LIBRA_ERR_NULL;
     if (!aligned_to(logits, dtype_bytes(dtype)) || (targets && !aligned_to(targets, index_bytes(index_type))) || !aligned_to(target_out, 4) || !aligned_to(entropy, 4) ||
@@ -847,7 +849,7 @@ extern "C" int libra_log_probs_backward(const void *logits, int64_t n, int64_t c
     if (int rc = shape(n, classes, top)) return rc;
     if (ld < classes || ld_dlogits < classes) return LIBRA_ERR_SHAPE;
     if (!known_dtype(dtype)) return LIBRA_ERR_DTYPE;
-    if ((targets && !known_index(index_type)) || !(scale > 0.f && std::isfinite(scale))) return LIBRA_ERR_OPTION;
+    if ((targets && !known_index(index_type)) || !known_scale(scale)) return LIBRA_ERR_OPTION;
     if (n == 0) return LIBRA_OK;
     if (!logits || !entropy || !stats || !dlogits || (d_target && !targets) || (top && d_top && !top_index)) return LIBRA_ERR_NULL;
     if (!aligned_to(logits, dtype_bytes(dtype)) || !aligned_to(dlogits, dtype_bytes(dtype)) || (targets && !aligned_to(targets, index_bytes(index_type))) ||

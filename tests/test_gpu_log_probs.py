@@ -416,3 +416,14 @@ def test_products_with_the_scale_are_formed_in_fp32(dtype, n, classes):
     assert r.top_index[:, 1].tolist() == [0] * n
     a = torch.stack([torch.zeros_like(d), d], 1)
     assert torch.equal(lb.log_probs_backward(x, r, None, None, None, a, scale=scale)[:, 0], (d * scale).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("classes", [30, 3000, 60000])
+def test_the_largest_scale(dtype, classes):
+    """2^127; twice that times log2 e is infinite, and it is refused."""
+    x = (logits(4, classes, torch.float32) * 2.0 ** -122).to(dtype)
+    check(x, targets_of(4, classes), min(classes, 4), 2.0 ** 127, gradient=False)
+    for scale in (1.8e38, 3.4e38):
+        with pytest.raises(lb.LibraError):
+            lb.log_probs(x, scale=scale)

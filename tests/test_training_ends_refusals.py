@@ -196,3 +196,9 @@ def test_a_row_beside_the_columns_that_are_written():
     assert apart > 300
     with pytest.raises(ValueError, match="overlaps"):
         lb._apart(held.view(24, 8)[1:3], held[:, :8], "t")          # rows of other distances: not looked at any further
+
+
+def test_the_largest_scale():
+    for scale in (1.8e38, 3e38):
+        assert log_probs(scale=scale) == E["OPTION"] and log_probs_backward(scale=scale) == E["OPTION"]
+    assert log_probs(scale=2.0 ** 127, n=0) == OK
