@@ -242,3 +242,53 @@ def test_the_widest_row():
     assert torch.equal(got[0], table[0]) and not bool(got[1].any())
     del table, got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n,rows,width,dtype", [(150001, 20000, 37, torch.float16), (20000, (1 << 22) + 5, 8, torch.bfloat16), (40000, 300, 520, torch.float32)])
+def test_the_gradient_of_many_ids_replayed_from_a_graph(n, rows, width, dtype):
+    """Other ids in every replay: no count, sum or row of zeros stays from the one before.  More tiles than a block adds up by itself, three
+    passes of the sort, rows of several workgroups."""
+    dout = torch.randn(n, width, device="cuda").to(dtype)
+    ids = ids_of(n, rows, "hot")
+    lb.embedding_backward(dout, ids, rows, SCALE)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grad = lb.embedding_backward(dout, ids, rows, SCALE)
+    for seed, kind in enumerate(("one", "uniform", "padding", "ends", "hot", "ordered", "one")):
+        ids.copy_(ids_of(n, rows, kind, seed=seed))
+        dout.normal_()
+        graph.replay()
+        want = lb.embedding_backward(dout, ids, rows, SCALE)
+        torch.cuda.synchronize()
+        assert torch.equal(grad, want), kind
+        if seed % 3 == 0:
+            check_gradient(grad, dout, ids, rows)
+
+
+def test_two_graphs_and_two_streams_of_many_ids():
+    """Workspaces of calls that run at the same time, eager ones and replayed ones."""
+    cases = []
+    for seed, (n, rows) in enumerate(((200000, 70000), (140000, 3000))):
+        ids = ids_of(n, rows, ("hot", "uniform")[seed], seed=seed)
+        cases.append((torch.randn(n, 64, device="cuda").half(), ids, rows))
+    want = [lb.embedding_backward(*c) for c in cases]
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in cases], []
+    for graph, c in zip(graphs, cases):
+        with torch.cuda.graph(graph):
+            outs.append(lb.embedding_backward(*c))
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(4):
+        for o in outs:
+            o.fill_(1)
+        torch.cuda.synchronize()
+        eager = []
+        for c, s, graph in zip(cases, streams, graphs):
+            with torch.cuda.stream(s):
+                eager.append(lb.embedding_backward(*c))
+                graph.replay()
+                eager.append(lb.embedding_backward(*c))
+        torch.cuda.synchronize()
+        for k, w in enumerate(want):
+            assert torch.equal(outs[k], w) and torch.equal(eager[2 * k], w) and torch.equal(eager[2 * k + 1], w)
