@@ -30,7 +30,6 @@ struct Tensors {                    // of one launch, in its arguments: nothing 
     libra_adamw_tensor_t t[LAUNCH_TENSORS];
     int32_t first[LAUNCH_TENSORS];  // workgroup that each begins with
     int64_t begin[LAUNCH_TENSORS];  // and the workgroup of the tensor that this one is
-    int32_t count;
 };
 
 struct Step {
@@ -358,17 +357,17 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
     for (int dtype = LIBRA_F16; dtype <= LIBRA_F32; ++dtype) {
         Tensors list;
         int64_t blocks = 0;
-        list.count = 0;
+        int listed = 0;
         auto launch = [&]() {
-            if (!list.count) return LIBRA_OK;
-            for (int j = list.count; j < LAUNCH_TENSORS; ++j) list.first[j] = INT32_MAX;
+            if (!listed) return LIBRA_OK;
+            for (int j = listed; j < LAUNCH_TENSORS; ++j) list.first[j] = INT32_MAX;
             const int rc = for_dtype(dtype, [&](auto tag) {
                 typedef decltype(tag) T;
                 if (bits8) hipLaunchKernelGGL((adamw_kernel<T, true>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, list, s);
                 else hipLaunchKernelGGL((adamw_kernel<T, false>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, list, s);
                 return last_launch();
             });
-            list.count = 0;
+            listed = 0;
             blocks = 0;
             return rc;
         };
@@ -377,12 +376,12 @@ extern "C" int libra_adamw(const libra_adamw_tensor_t *tensors, int32_t count, c
             const libra_adamw_tensor_t &t = tensors[k];
             const int64_t all = (t.n + GROUP_BLOCKS * STATE_BLOCK - 1) / (GROUP_BLOCKS * STATE_BLOCK);
             for (int64_t begin = 0; begin < all;) {
-                if (list.count == LAUNCH_TENSORS || blocks == LAUNCH_BLOCKS)
+                if (listed == LAUNCH_TENSORS || blocks == LAUNCH_BLOCKS)
                     if (int rc = launch()) return rc;
                 const int64_t some = std::min(all - begin, LAUNCH_BLOCKS - blocks);
-                list.t[list.count] = t;
-                list.first[list.count] = (int32_t)blocks;
-                list.begin[list.count++] = begin;
+                list.t[listed] = t;
+                list.first[listed] = (int32_t)blocks;
+                list.begin[listed++] = begin;
                 blocks += some;
                 begin += some;
             }
