@@ -378,8 +378,9 @@ int libra_embedding(const void *table, int64_t rows, int32_t width, int64_t ld_t
 
 /*
  * libra_embedding_backward - dtable[v,:] = scale * sum over all i with index[i] = v of dout[i,:]: the ids are sorted, the rows of an id
- * are added in fp32, the sum is rounded once to `dtype`.  The order of additions depends on the ids and n alone, so equal calls give
- * equal bits.  Rows that no id names become zeros; ids outside [0, rows) count for nothing.
+ * are added in fp32, the sum times scale is formed in fp32 and rounded once to `dtype`.  The order of additions depends on the ids, n, rows,
+ * width and dtype, and on nothing else: equal calls give equal bits, a part of the columns or a longer table need not.  Rows that no id
+ * names become zeros; ids outside [0, rows) count for nothing.
  *   dout       device, n x width with row stride ld_dout, width <= 2^21;  index as in libra_embedding;  n < 2^31
  *   dtable     device, rows x width with row stride ld_dtable, rows < 2^31 - 1; fully overwritten; none of the inputs
  *   workspace  device, 256-byte aligned, libra_embedding_backward_workspace() bytes, not needed after the call has run (n = 0: may be NULL)
@@ -400,7 +401,8 @@ int libra_embedding_backward(const void *dout, int64_t ld_dout, int dtype, const
  *   stats      device, fp32[2 n]: the largest logit and log sum exp(scale * (x - largest)) of each row, for the backward call
  *   workspace  device, 256-byte aligned, libra_log_probs_workspace() bytes (0: may be NULL), not needed after the call has run
  * A logit of -Inf is a class of probability 0.  A row of nothing else has no distribution: log probabilities -Inf, entropy 0, gradient 0.
- * A row with a NaN or +Inf has NaN for all of its numbers; NaN counts as the largest logit.
+ * A row with a NaN or +Inf has NaN for all of its numbers (but 0 for a target of -1); NaN counts as the largest logit.  The entropy's sum
+ * of p_j (x_j - largest) is formed before it is scaled and has to stay within fp32: logits within 2^127 / classes always do.
  * Errors: NULL, SHAPE, TOO_LARGE, UNSUPPORTED (top), DTYPE, OPTION (index_type, scale), BUFFER, HIP.
  */
 #define LIBRA_LOG_PROBS_MAX_TOP 64
@@ -430,7 +432,8 @@ int libra_log_probs_backward(const void *logits, int64_t n, int64_t classes, int
  * second_scales) for every LIBRA_ADAMW_BLOCK elements, the smallest that keeps the block's largest finite number within 448 (at least
  * 2^-126).  The numbers that they stand for are rounded up or down to a neighbour by chance:
  *   y = |x| / scale, e = max(exponent of y, -6), q = floor(y * 2^(3 - e) + chance), code = 8 (e + 6) + q
- * with at least q = 1 for a root above 0; Inf and NaN become code 127.  The chance of element i of tensor `number`: h = mix(key + (low
+ * with at least q = 1 for a root above 0; Inf and NaN become code 127.  (Rounding the root without bias leaves v with its variance on top: the
+ * roots are about 1 % larger than those of 32-bit states.)  The chance of element i of tensor `number`: h = mix(key + (low
  * word of i) + (high word of i) * 0x9E3779B1), key = mix(mix(mix(seed) + t) + number), all modulo 2^32; (h mod 2^16) / 2^16 for m, (h div
  * 2^16) / 2^16 for the root; mix(x): x ^= x >> 16, x *= 0x6C8E9CF5, x ^= x >> 15, x *= 0x58AC4D6B, x ^= x >> 16.  The same step gives
  * the same bits every time.

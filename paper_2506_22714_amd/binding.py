@@ -902,7 +902,8 @@ def embedding(table, index, scale: float = 1.0, out=None):
 
 def embedding_backward(dout, index, rows: int, scale: float = 1.0, out=None):
     """Gradient of ``embedding(table, index, scale)`` with respect to a table of ``rows`` rows, from the gradient ``dout`` (a row per id)
-    of its result: rows of equal ids are added in fp32, in an order that depends on the ids alone, and rounded once to dout's type."""
+    of its result: rows of equal ids are added in fp32, in an order that depends on the ids, the shapes and the type alone, and rounded once
+    to dout's type."""
     torch = _gpu()
     dtype = _rows_of(dout, "dout")
     kind = _index_code(index, "index", dout)

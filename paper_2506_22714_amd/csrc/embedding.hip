@@ -12,7 +12,8 @@ namespace {
 
 // What a lane moves of a row: 16 bytes at a multiple of 16; 16 bytes anywhere, where rows are not aligned (the last piece of a row then ends
 // with the row and overlaps the one before: both lanes hold and write the same numbers there); an element, where rows are shorter.
-// (Elements instead of 16 bytes anywhere: lookup of 1,000,003 rows of 63 bf16 85 us, not 57, their gradient 181, not 153.)
+// (Elements instead of 16 bytes anywhere: lookup of 1,000,003 rows of 63 bf16 85 us, not 57, their gradient 181, not 153.  Rows of 64 take 44: one
+// of 126 bytes lies on two lines of memory, and 212 MiB come from it, not 110.)
 enum Access { ELEMENTS, ANYWHERE, ALIGNED };
 
 template <class T, int ACCESS> struct Piece {
