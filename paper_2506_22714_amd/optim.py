@@ -108,7 +108,7 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p][name] = x.detach().to(p.device, copy=True)
         filled = {}                     # groups may share a rate, as long as what is loaded is the same
         for g, rate in zip(self.param_groups, rates):
-            device = g["params"][0].device
+            device = g["params"][0].device if g["params"] else "cpu"
             if isinstance(g.get("step"), torch.Tensor):
                 g["step"] = g["step"].to(device)
             if isinstance(g["lr"], torch.Tensor):

@@ -202,3 +202,16 @@ def test_the_largest_scale():
     for scale in (1.8e38, 3e38):
         assert log_probs(scale=scale) == E["OPTION"] and log_probs_backward(scale=scale) == E["OPTION"]
     assert log_probs(scale=2.0 ** 127, n=0) == OK
+
+
+def test_a_checkpoint_of_a_group_without_parameters():
+    from paper_2506_22714_amd.optim import AdamW
+    make = lambda lr: AdamW([{"params": [torch.nn.Parameter(torch.zeros(4))]}, {"params": [], "lr": lr}])      # noqa: E731
+    again = make(0.5)
+    again.load_state_dict(make(0.25).state_dict())
+    assert [g["lr"] for g in again.param_groups] == [1e-3, 0.25]
+    rate = torch.full((1,), 0.125)
+    make_tensor = lambda lr: AdamW([{"params": [torch.nn.Parameter(torch.zeros(4))]}, {"params": [], "lr": lr}], capturable=True)      # noqa: E731
+    again = make_tensor(torch.zeros(1))
+    again.load_state_dict(make_tensor(rate).state_dict())
+    assert float(again.param_groups[1]["lr"]) == 0.125
