@@ -58,6 +58,8 @@ class AdamW(torch.optim.Optimizer):
                 # parameters whose gradients came and went may stand at different steps: one call for each of them.  The tensor's number, by
                 # which 8-bit states draw their chances, is its place among all parameters, whoever has a gradient
                 calls = {}
+                if not group["params"]:
+                    continue
                 if group["capturable"] and "step" not in group:
                     self._not_captured()
                     group["step"] = torch.zeros((), dtype=torch.int64, device=group["params"][0].device)

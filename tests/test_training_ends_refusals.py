@@ -215,3 +215,15 @@ def test_a_checkpoint_of_a_group_without_parameters():
     again = make_tensor(torch.zeros(1))
     again.load_state_dict(make_tensor(rate).state_dict())
     assert float(again.param_groups[1]["lr"]) == 0.125
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_step_of_a_group_without_parameters(capturable, monkeypatch):
+    """It has no GPU to count on."""
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    from paper_2506_22714_amd.optim import AdamW
+    opt = AdamW([{"params": []}, {"params": [torch.nn.Parameter(torch.zeros(4))]}], capturable=capturable)
+    for _ in range(2):
+        opt.step()                      # no parameter has a gradient
+    if capturable:
+        assert int(opt.param_groups[1]["step"]) == 2 and "step" not in opt.param_groups[0]
