@@ -402,7 +402,7 @@ int libra_embedding_backward(const void *dout, int64_t ld_dout, int dtype, const
  *   workspace  device, 256-byte aligned, libra_log_probs_workspace() bytes (0: may be NULL), not needed after the call has run
  * A logit of -Inf is a class of probability 0.  A row of nothing else has no distribution: log probabilities -Inf, entropy 0, gradient 0.
  * A row with a NaN or +Inf has NaN for all of its numbers (but 0 for a target of -1); NaN counts as the largest logit.  The entropy's sum
- * of p_j (x_j - largest) is formed before it is scaled and has to stay within fp32: logits within 2^127 / classes always do.
+ * of p_j (x_j - largest) is formed before it is scaled and has to stay within fp32: logits within 2^126 / classes always do.
  * Errors: NULL, SHAPE, TOO_LARGE, UNSUPPORTED (top), DTYPE, OPTION (index_type, scale), BUFFER, HIP.
  */
 #define LIBRA_LOG_PROBS_MAX_TOP 64
